@@ -377,6 +377,89 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
                              double top_p, uint64_t rng_seed, uint64_t rng_step, int32_t *out_tokens,
                              int32_t *out_kept, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * sbw_token_logprobs -- log probabilities of given tokens, with what goes with an answer: the
+ * entropy of each row, the token's rank and the row's most probable alternatives, in one pass over
+ * read-only logits and one launch.  (The paper scores texts by perplexity, Table 5; a server
+ * returns these numbers beside the sampled tokens; an entropy-weighted detector takes the
+ * entropies, see sbw_detect_weighted.)  Per row b, with l' the biased logits of Eq. 2 in the logits'
+ * own precision -- the logits themselves where delta is 0 in it -- tau = temperature, t = tokens[b]:
+ *     m = max_v l'_v        Z = sum_v exp((l'_v - m) / tau)        (as sbw_bias_sample returns them)
+ *     log p_v = (l'_v - m) / tau - ln Z
+ *     logprob = log p_t     entropy = - sum_v p_v log p_v  (in nats; 0 log 0 = 0)
+ *     rank    = 1 + #{v : l'_v > l'_t} + #{v < t : l'_v = l'_t}
+ *     alternatives: the top_n first columns by l' descending, ties to the lowest column (a token
+ *     of rank r <= top_n is alternative r - 1), and their log p.
+ * For this order -0 equals +0 and NaN counts as -inf.
+ *
+ *   logits, dtype, B, V, ld, vocab_offset, key, gamma, scheme   as for sbw_bias_sample; rows of any
+ *                 alignment take the vectorised path.
+ *   ctx_tokens, ctx_width   as for sbw_bias_sample; ctx_tokens may be NULL where delta is 0.
+ *   delta         0: no watermark (nothing is hashed).
+ *   tokens        device [B] int32 column indices (0-based within this shard, as sbw_bias_sample
+ *                 returns them), or NULL: no out_logprob and no out_rank then.  A token outside
+ *                 [0, V) marks a padded row: its logits do not count, its outputs are 0, its
+ *                 alternatives ids -1 with log probability -inf.
+ *   top_n         0 .. SBW_MAX_TOP_LOGPROBS (SBW_ERR_TOO_LARGE beyond).  With top_n > V the places
+ *                 from V on are id -1, log probability -inf.
+ *   out_logprob, out_entropy, out_max, out_sumexp   device [B] float;  out_rank  device [B] int32;
+ *   out_top_ids, out_top_logprobs   device [B, top_n] int32 / float.  Each may be NULL, not all.
+ * A row whose logits are all -inf: every log p is -inf, entropy 0, m -inf, Z 0.  A row with a NaN or
+ * +inf among its biased logits: logprob, entropy, m, Z and the alternatives' log p are NaN.
+ * Statistics are fp32 sums of fp32 exponentials in a chain of at most 48 additions (V <= 2^18, one
+ * more per 16384 columns beyond), merged in fp64: log p is within 8e-6 + 2^-21 (H + |log p|) of its exact value,
+ * the entropy H within 16e-6 (1 + H); a tenth of that is usual.  The
+ * order of the sums is fixed by the shape: equal calls give equal bits.  No workspace; calls on
+ * different streams may overlap.  V <= 2^31 - 1.
+ *
+ * sbw_token_logprobs_backward -- the gradient of those log probabilities and entropies with respect
+ * to the logits (straight through the watermark's addition: d l'_v / d l_v = 1):
+ *     d_v = (1/tau) [ g (1[v = t] - p_v) - h p_v (log p_v + H) ],  g = grad_logprob[b], h = grad_entropy[b]
+ * with p_v = exp((l'_v - m) / tau) / Z and H the saved entropy.
+ *   max, sumexp, entropy   device [B] float: m, Z, H of the forward call (m and Z may come from
+ *                 sbw_bias_sample too); entropy may be NULL where grad_entropy is.
+ *   grad_logprob, grad_entropy   device [B] float; one of them may be NULL (0).  tokens may be NULL
+ *                 where grad_logprob is.
+ *   grad_logits   device [B, grad_ld] of `dtype`: every element of columns 0 .. V-1 is written, the
+ *                 rest of a row is not; rounded once.  It may be `logits` itself (grad_ld = ld): the gradient then
+ *                 takes the logits' place.  Any other overlap of the two is SBW_ERR_INVALID_ARG.
+ * Padded rows and rows whose logits are all -inf get zeros; rows with NaN or +inf get NaN.  p_v is an
+ * fp32 exponential: relative error below 2^-21 + 2^-22 (m - l'_v) / tau (below 2^-126 it is 0).
+ */
+#define SBW_MAX_TOP_LOGPROBS 64
+int sbw_token_logprobs(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld, int64_t vocab_offset,
+                       const int32_t *ctx_tokens, int ctx_width, uint64_t key, double gamma, float delta,
+                       int scheme, float temperature, const int32_t *tokens, int64_t top_n,
+                       float *out_logprob, float *out_entropy, int32_t *out_rank, float *out_max,
+                       float *out_sumexp, int32_t *out_top_ids, float *out_top_logprobs, void *stream);
+int sbw_token_logprobs_backward(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld,
+                                int64_t vocab_offset, const int32_t *ctx_tokens, int ctx_width, uint64_t key,
+                                double gamma, float delta, int scheme, float temperature,
+                                const int32_t *tokens, const float *max, const float *sumexp,
+                                const float *entropy, const float *grad_logprob, const float *grad_entropy,
+                                void *grad_logits, int64_t grad_ld, void *stream);
+
+/*
+ * sbw_detect_weighted -- sbw_detect with a weight per token (entropy-weighted detection: positions
+ * where the model had a choice say more than positions where it had none; 0/1 weights score a
+ * chosen part of a text).  Over the scored positions i of a sequence, with Y_i as for sbw_detect:
+ *     G = sum w_i Y_i     S1 = sum w_i     S2 = sum w_i^2     (fp64)
+ *     z = (G - gamma S1) / sqrt(S2 gamma (1 - gamma));  S2 = 0 gives z = 0.
+ * With every weight 1 this is sbw_detect's z, bit for bit.
+ *   weights     device [total_tokens] float, one per token of `tokens`, in its place; those of the
+ *               first ctx_width tokens of a sequence are not read into any sum.  Any finite value; a
+ *               NaN or an infinity among a sequence's scored weights makes its z NaN.
+ *   out_green, out_weight, out_weight2   device [N] double: G, S1, S2; each may be NULL.
+ *   out_z       device [N] double.
+ * Other arguments, lengths, offsets and workspace as for sbw_detect
+ * (sbw_detect_workspace_bytes(N) where offsets is NULL).  The order of the sums is fixed by N, the
+ * lengths and total_tokens: equal calls give equal bits.
+ */
+int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32_t *lengths,
+                        const int64_t *offsets, int64_t N, int64_t total_tokens, int ctx_width, uint64_t key,
+                        double gamma, int scheme, double *out_green, double *out_weight, double *out_weight2,
+                        double *out_z, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,6 +107,14 @@ def lib() -> ctypes.CDLL:
         L.sbw_oracle_bias_sample_filtered.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double,
                                                       c.c_float, i32, c.c_float, i64, c.c_double, u64, u64,
                                                       vp, vp, vp, i32]
+        L.sbw_oracle_token_logprobs.restype = None
+        L.sbw_oracle_token_logprobs.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double, c.c_float,
+                                                i32, c.c_float, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32]
+        L.sbw_oracle_token_logprobs_backward.restype = None
+        L.sbw_oracle_token_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double,
+                                                         c.c_float, i32, c.c_float, vp, vp, vp, vp, vp, vp, vp, i32]
+        L.sbw_oracle_detect_weighted.restype = None
+        L.sbw_oracle_detect_weighted.argtypes = [vp, vp, vp, i64, i32, u64, c.c_double, i32, vp, vp, vp, vp]
         L.sbw_oracle_jenkins_collisions.restype = i64
         L.sbw_oracle_jenkins_collisions.argtypes = []
         L.sbw_oracle_log_max_ulp.restype = c.c_double
@@ -317,6 +325,54 @@ def bias_sample_filtered(logits: np.ndarray, V, ctx_tokens, key, gamma, delta, s
                                           delta, scheme, temperature, top_k, top_p, rng_seed, rng_step,
                                           _ptr(tokens), _ptr(kept), _ptr(mask), threads)
     return {"tokens": tokens, "kept": kept, "mask": mask}
+
+
+def token_logprobs(logits: np.ndarray, V, tokens, temperature, top_n=0, ctx_tokens=None, key=0, gamma=0.5,
+                   delta=0.0, scheme=SCHEME_CONTEXT, vocab_offset=0, threads=8):
+    """Log probabilities, entropies, ranks, softmax statistics and alternatives in fp64: dict of arrays."""
+    assert logits.ndim == 2 and logits.dtype in (np.float32, np.uint16)
+    x = np.ascontiguousarray(logits)
+    B, ld = x.shape
+    ctx, W = (None, 1) if ctx_tokens is None else _ctx(ctx_tokens, B)
+    tok = None if tokens is None else np.ascontiguousarray(np.asarray(tokens, dtype=np.int32))
+    f = lambda *shape: np.zeros(shape, dtype=np.float64)   # noqa: E731
+    out = {"logprob": f(B), "entropy": f(B), "rank": np.zeros(B, dtype=np.int32), "max": f(B), "sumexp": f(B),
+           "top_ids": np.zeros((B, top_n), dtype=np.int32), "top_logprobs": f(B, top_n)}
+    lib().sbw_oracle_token_logprobs(_ptr(x), DTYPE_F32 if x.dtype == np.float32 else DTYPE_BF16, B, V, ld,
+                                    vocab_offset, _ptr(ctx), W, key, gamma, delta, scheme, temperature, _ptr(tok),
+                                    top_n, *(_ptr(out[k]) for k in ("logprob", "entropy", "rank", "max", "sumexp",
+                                                                    "top_ids", "top_logprobs")), threads)
+    return out
+
+
+def token_logprobs_backward(logits: np.ndarray, V, tokens, temperature, m, Z, H, grad_logprob=None,
+                            grad_entropy=None, ctx_tokens=None, key=0, gamma=0.5, delta=0.0,
+                            scheme=SCHEME_CONTEXT, vocab_offset=0, threads=8) -> np.ndarray:
+    """Gradient of log probability and entropy with respect to the biased logits: [B, V] float64."""
+    x = np.ascontiguousarray(logits)
+    B, ld = x.shape
+    ctx, W = (None, 1) if ctx_tokens is None else _ctx(ctx_tokens, B)
+    tok = None if tokens is None else np.ascontiguousarray(np.asarray(tokens, dtype=np.int32))
+    d = lambda a: None if a is None else np.ascontiguousarray(np.asarray(a, dtype=np.float64))   # noqa: E731
+    m, Z, H, g, h = d(m), d(Z), d(H), d(grad_logprob), d(grad_entropy)
+    out = np.zeros((B, V), dtype=np.float64)
+    lib().sbw_oracle_token_logprobs_backward(_ptr(x), DTYPE_F32 if x.dtype == np.float32 else DTYPE_BF16, B, V, ld,
+                                             vocab_offset, _ptr(ctx), W, key, gamma, delta, scheme, temperature,
+                                             _ptr(tok), _ptr(m), _ptr(Z), _ptr(H), _ptr(g), _ptr(h), _ptr(out),
+                                             threads)
+    return out
+
+
+def detect_weighted(tokens, weights, lengths, key, gamma, scheme, ctx_width=1):
+    """Weighted detection: (G, S1, S2, z), float64 per sequence."""
+    tok = np.ascontiguousarray(np.asarray(tokens, dtype=np.int32))
+    w = np.ascontiguousarray(np.asarray(weights, dtype=np.float32))
+    lens = np.ascontiguousarray(np.asarray(lengths, dtype=np.int32))
+    N = lens.shape[0]
+    G, S1, S2, z = (np.zeros(N, dtype=np.float64) for _ in range(4))
+    lib().sbw_oracle_detect_weighted(_ptr(tok), _ptr(w), _ptr(lens), N, ctx_width, key, gamma, scheme, _ptr(G),
+                                     _ptr(S1), _ptr(S2), _ptr(z))
+    return G, S1, S2, z
 
 
 def jenkins_collisions() -> int:

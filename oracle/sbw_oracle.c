@@ -728,6 +728,180 @@ void sbw_oracle_bias_sample_filtered(const void *logits, int dtype, int64_t B, i
     }
 }
 
+/* ------------------------------------------------------- log probabilities of tokens ---- */
+/* The row's biased logits as doubles (exact). */
+static void biased_row(const void *logits, int dtype, int64_t b, int64_t V, int64_t ld, int64_t vocab_offset,
+                       const int32_t *ctx, int W, uint64_t key, uint64_t thr, float delta, int scheme, double *x)
+{
+    const int marked = delta != 0.0f;                  /* ctx may be NULL where nothing is added */
+    for (int64_t j = 0; j < V; ++j) {
+        int g = 0;
+        if (marked) {
+            uint32_t v = (uint32_t)(vocab_offset + j);
+            g = sbw_oracle_green(seed_for(scheme, key, ctx, W, v), v, thr);
+        }
+        if (dtype == SBW_O_DTYPE_BF16)
+            x[j] = sbw_oracle_bf16_to_f32(sbw_oracle_bias_elem_bf16(((const uint16_t *)logits)[b * ld + j], delta, g));
+        else
+            x[j] = sbw_oracle_bias_elem_f32(((const float *)logits)[b * ld + j], delta, g);
+    }
+}
+
+typedef struct {
+    double value;
+    int64_t col;
+} choice_t;
+
+static int choice_cmp(const void *pa, const void *pb)
+{
+    const choice_t *a = (const choice_t *)pa, *b = (const choice_t *)pb;
+    if (a->value != b->value)
+        return a->value > b->value ? -1 : 1;
+    return a->col < b->col ? -1 : a->col > b->col;
+}
+
+void sbw_oracle_token_logprobs(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld,
+                               int64_t vocab_offset, const int32_t *ctx_tokens, int ctx_width,
+                               uint64_t key, double gamma, float delta, int scheme, float temperature,
+                               const int32_t *tokens, int64_t top_n, double *out_logprob,
+                               double *out_entropy, int32_t *out_rank, double *out_max,
+                               double *out_sumexp, int32_t *out_top_ids, double *out_top_logprobs,
+                               int threads)
+{
+    const uint64_t thr = sbw_oracle_threshold(gamma);
+    const double tau = (double)temperature;
+    if (threads < 1)
+        threads = 1;
+#pragma omp parallel for num_threads(threads) schedule(dynamic, 1)
+    for (int64_t b = 0; b < B; ++b) {
+        int64_t t = tokens ? (int64_t)tokens[b] : 0;
+        double lp = 0.0, H = 0.0, m = 0.0, Z = 0.0;
+        int64_t rank = 0;
+        for (int64_t i = 0; i < top_n; ++i) {
+            out_top_ids[b * top_n + i] = -1;
+            out_top_logprobs[b * top_n + i] = -INFINITY;
+        }
+        if (!tokens || (t >= 0 && t < V)) {
+            double *x = (double *)malloc((size_t)V * sizeof(double));
+            choice_t *order = (choice_t *)malloc((size_t)V * sizeof(choice_t));
+            biased_row(logits, dtype, b, V, ld, vocab_offset, ctx_tokens ? ctx_tokens + b * ctx_width : NULL,
+                       ctx_width, key, thr, delta, scheme, x);
+            int bad = 0;
+            m = -INFINITY;
+            for (int64_t j = 0; j < V; ++j) {
+                if (x[j] != x[j] || x[j] == INFINITY)
+                    bad = 1;
+                if (x[j] > m)
+                    m = x[j];
+            }
+            if (bad) {
+                m = Z = H = NAN;
+            } else if (m > -INFINITY) {
+                long double sum = 0.0L, first = 0.0L;
+                for (int64_t j = 0; j < V; ++j) {
+                    double d = (x[j] - m) / tau;
+                    long double e = expl((long double)d);
+                    sum += e;
+                    if (e > 0.0L)
+                        first += e * d;
+                }
+                Z = (double)sum;
+                H = (double)(logl(sum) - first / sum);
+            }
+            /* a log probability: -inf everywhere in a row of -inf, NaN in a bad row */
+#define LOGP(v) (bad ? NAN : m == -INFINITY ? -INFINITY : ((v) - m) / tau - log(Z))
+            lp = LOGP(x[t]);
+            double xt = x[t] == x[t] ? x[t] : -INFINITY;
+            rank = 1;
+            for (int64_t j = 0; j < V; ++j) {
+                double v = x[j] == x[j] ? x[j] : -INFINITY;
+                rank += v > xt || (v == xt && j < t);
+                order[j].value = v;
+                order[j].col = j;
+            }
+            if (top_n > 0) {
+                qsort(order, (size_t)V, sizeof(choice_t), choice_cmp);
+                for (int64_t i = 0; i < top_n && i < V; ++i) {
+                    out_top_ids[b * top_n + i] = (int32_t)order[i].col;
+                    out_top_logprobs[b * top_n + i] = LOGP(order[i].value);
+                }
+            }
+#undef LOGP
+            free(order);
+            free(x);
+        }
+        if (tokens) {
+            out_logprob[b] = lp;
+            out_rank[b] = (int32_t)rank;
+        }
+        out_entropy[b] = H;
+        out_max[b] = m;
+        out_sumexp[b] = Z;
+    }
+}
+
+void sbw_oracle_token_logprobs_backward(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld,
+                                        int64_t vocab_offset, const int32_t *ctx_tokens, int ctx_width,
+                                        uint64_t key, double gamma, float delta, int scheme,
+                                        float temperature, const int32_t *tokens, const double *m,
+                                        const double *Z, const double *H, const double *g,
+                                        const double *h, double *out_grad, int threads)
+{
+    const uint64_t thr = sbw_oracle_threshold(gamma);
+    const double tau = (double)temperature;
+    if (threads < 1)
+        threads = 1;
+#pragma omp parallel for num_threads(threads) schedule(dynamic, 1)
+    for (int64_t b = 0; b < B; ++b) {
+        const int64_t t = tokens ? (int64_t)tokens[b] : -1;
+        double *out = out_grad + b * V;
+        if ((tokens && (t < 0 || t >= V)) || Z[b] == 0.0) {       /* padded, or every logit -inf */
+            for (int64_t j = 0; j < V; ++j)
+                out[j] = 0.0;
+            continue;
+        }
+        double *x = (double *)malloc((size_t)V * sizeof(double));
+        biased_row(logits, dtype, b, V, ld, vocab_offset, ctx_tokens ? ctx_tokens + b * ctx_width : NULL,
+                   ctx_width, key, thr, delta, scheme, x);
+        for (int64_t j = 0; j < V; ++j) {
+            const double d = (x[j] - m[b]) / tau, p = exp(d) / Z[b];
+            double grad = g ? -g[b] * p : 0.0;
+            if (h && p != 0.0)                                     /* p log p -> 0 */
+                grad -= h[b] * p * (d - log(Z[b]) + H[b]);
+            if (g && j == t)
+                grad += g[b];
+            out[j] = grad / tau;
+        }
+        free(x);
+    }
+}
+
+void sbw_oracle_detect_weighted(const int32_t *tokens, const float *weights, const int32_t *lengths,
+                                int64_t N, int ctx_width, uint64_t key, double gamma, int scheme,
+                                double *green, double *weight, double *weight2, double *z)
+{
+    const uint64_t thr = sbw_oracle_threshold(gamma);
+    int64_t start = 0;
+    for (int64_t s = 0; s < N; ++s) {
+        const int64_t L = lengths[s] > 0 ? lengths[s] : 0;
+        const int32_t *tok = tokens + start;
+        long double G = 0.0L, S1 = 0.0L, S2 = 0.0L;
+        for (int64_t t = ctx_width; t < L; ++t) {
+            const uint32_t v = (uint32_t)tok[t];
+            const long double w = weights[start + t];
+            if (sbw_oracle_green(seed_for(scheme, key, tok + (t - ctx_width), ctx_width, v), v, thr))
+                G += w;
+            S1 += w;
+            S2 += w * w;
+        }
+        green[s] = (double)G;
+        weight[s] = (double)S1;
+        weight2[s] = (double)S2;
+        z[s] = S2 == 0.0L ? 0.0 : (double)((G - gamma * S1) / sqrtl(S2 * gamma * (1.0L - gamma)));
+        start += L;
+    }
+}
+
 /* ------------------------------------------------------------------ exhaustive checks */
 int64_t sbw_oracle_jenkins_collisions(void)
 {

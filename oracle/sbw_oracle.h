@@ -25,6 +25,9 @@
  *   sample             softmax, scipy softmax / logsumexp, closed form
  *   top-k / top-p      pinned: fp64 softmax + cumulative sums (numpy), torch.topk,  (test_oracle_filter)
  *   sampling           2^f in fp64, closed forms, chi-square of sampled ids
+ *   token_logprobs,    pinned: scipy log_softmax / entropy, brute-force ranks,   (test_oracle_logprob)
+ *   its gradient       torch autograd in fp64, central differences
+ *   detect_weighted    pinned: the plain detector at weight 1, brute force sums  (test_oracle_logprob)
  *   bit compatibility with the paper authors' own package: PARITY UNPINNED (the paper
  *   prints no hash input/output pair; the constants below are this library's frozen
  *   reading, "SBW-spec v1").
@@ -144,6 +147,32 @@ void sbw_oracle_bias_sample_filtered(const void *logits, int dtype, int64_t B, i
                                      float temperature, int64_t top_k, double top_p, uint64_t rng_seed,
                                      uint64_t rng_step, int32_t *out_tokens, int32_t *out_kept,
                                      uint8_t *out_mask, int threads);
+
+/* Log probabilities of given tokens under the softmax of the biased logits, in fp64: per row
+ * log p_t, entropy (nats), 1-based rank (value descending, lowest column first among equals; NaN
+ * counts as -inf, -0 equals +0), m = max, Z = sum exp((l - m)/tau), and the top_n first columns in that
+ * order with their log p.  tokens may be NULL (no logprob, no rank).  A token outside [0, V): all 0,
+ * ids -1, log p -inf.  All -inf: log p -inf, entropy 0, m -inf, Z 0.  NaN or +inf: NaN. */
+void sbw_oracle_token_logprobs(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld,
+                               int64_t vocab_offset, const int32_t *ctx_tokens, int ctx_width,
+                               uint64_t key, double gamma, float delta, int scheme, float temperature,
+                               const int32_t *tokens, int64_t top_n, double *out_logprob,
+                               double *out_entropy, int32_t *out_rank, double *out_max,
+                               double *out_sumexp, int32_t *out_top_ids, double *out_top_logprobs,
+                               int threads);
+/* Its gradient with respect to the biased logits, (1/tau)(g (1[v=t] - p_v) - h p_v (log p_v + H)), from
+ * given m, Z, H (one double each per row), into [B, V] doubles. */
+void sbw_oracle_token_logprobs_backward(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld,
+                                        int64_t vocab_offset, const int32_t *ctx_tokens, int ctx_width,
+                                        uint64_t key, double gamma, float delta, int scheme,
+                                        float temperature, const int32_t *tokens, const double *m,
+                                        const double *Z, const double *H, const double *g,
+                                        const double *h, double *out_grad, int threads);
+/* Weighted detection: G = sum w Y, S1 = sum w, S2 = sum w^2 over the scored positions,
+ * z = (G - gamma S1)/sqrt(S2 gamma (1 - gamma)), 0 where S2 is 0. */
+void sbw_oracle_detect_weighted(const int32_t *tokens, const float *weights, const int32_t *lengths,
+                                int64_t N, int ctx_width, uint64_t key, double gamma, int scheme,
+                                double *green, double *weight, double *weight2, double *z);
 
 /* Exhaustive checks that are too slow from Python; each returns a summary. */
 /* Number of 32-bit values hit more than once by jenkins over all 2^32 inputs (0 = bijection).

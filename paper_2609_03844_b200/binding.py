@@ -25,6 +25,7 @@ SCHEME_CONTEXT = 0
 SCHEME_SELFSALT = 1
 DTYPE_F32 = 0
 DTYPE_BF16 = 1
+MAX_TOP_LOGPROBS = 64
 
 EXPORTS = ("sbw_version", "sbw_last_cuda_error", "sbw_bias_logits",
            "sbw_bias_logits_host_staging_bytes", "sbw_bias_logits_host",
@@ -33,7 +34,8 @@ EXPORTS = ("sbw_version", "sbw_last_cuda_error", "sbw_bias_logits",
            "sbw_bias_sample_shard", "sbw_sample_combine", "sbw_detect_bits_words", "sbw_detect_bits",
            "sbw_window_z", "sbw_prefix_z", "sbw_detect_unique_workspace_bytes", "sbw_detect_unique",
            "sbw_roc_auc_workspace_bytes", "sbw_roc_auc", "sbw_sample_filtered_workspace_bytes",
-           "sbw_bias_sample_filtered", "sbw_roc_auc_batched", "sbw_bias_sample_shard_ids")
+           "sbw_bias_sample_filtered", "sbw_roc_auc_batched", "sbw_bias_sample_shard_ids",
+           "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted")
 
 _lib = None
 
@@ -137,6 +139,15 @@ def lib() -> ctypes.CDLL:
         L.sbw_bias_sample_filtered.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double,
                                                c.c_float, i32, c.c_float, i64, c.c_double, u64, u64, vp, vp,
                                                vp, sz, vp]
+        L.sbw_token_logprobs.restype = i32
+        L.sbw_token_logprobs.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double, c.c_float, i32,
+                                         c.c_float, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.sbw_token_logprobs_backward.restype = i32
+        L.sbw_token_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double, c.c_float,
+                                                  i32, c.c_float, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.sbw_detect_weighted.restype = i32
+        L.sbw_detect_weighted.argtypes = [vp, vp, vp, vp, i64, i64, i32, u64, c.c_double, i32, vp, vp, vp, vp, vp,
+                                          sz, vp]
         L.sbw_int_probe.restype = i32
         L.sbw_int_probe.argtypes = [i32, i32, i32, i32, vp, vp, vp]
         atexit.register(_drain_at_exit)
@@ -183,6 +194,53 @@ def _ctx(ctx_tokens: torch.Tensor, B: int) -> int:
     if ctx_tokens.numel() % B != 0 or ctx_tokens.numel() == 0:
         raise ValueError("ctx_tokens must hold B * ctx_width ids")
     return ctx_tokens.numel() // B
+
+
+def _expect(name: str, t: torch.Tensor | None, dtype: torch.dtype, n: int, device: torch.device) -> int | None:
+    """The address of a contiguous ``dtype`` tensor of ``n`` elements on ``device`` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor on {device}")
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+class _on:
+    """Makes ``device`` current for a call if it is not (launches go to the current device)."""
+
+    def __init__(self, device: torch.device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _logits_layout(name: str, t: torch.Tensor, V: int | None):
+    """``_row_layout`` for the calls that check their tensors' device: (B, V, ld)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    B, V, ld = _row_layout(t, V)
+    if not 0 < V <= t.shape[1]:
+        raise ValueError(f"V must lie in 1 .. {t.shape[1]}, got {V}")
+    return B, V, ld
+
+
+def _watermark(ctx_tokens: torch.Tensor | None, B: int, delta: float, device: torch.device):
+    """(address, width) of the context tokens; they may be left out where delta is 0."""
+    if ctx_tokens is None:
+        if delta != 0:
+            raise ValueError("ctx_tokens is needed where delta is not 0")
+        return None, 1
+    if ctx_tokens.device != device:
+        raise ValueError(f"ctx_tokens must be on {device}")
+    return ctx_tokens.data_ptr(), _ctx(ctx_tokens, B)
 
 
 def sbw_version() -> str:
@@ -480,6 +538,95 @@ def sbw_roc_auc_batched(z: torch.Tensor, labels: torch.Tensor, offsets: torch.Te
                                    _stream(stream))
     _check("sbw_roc_auc_batched", rc)
     return out_auc
+
+
+def sbw_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, temperature: float = 1.0, *,
+                       out_logprob: torch.Tensor | None = None, out_entropy: torch.Tensor | None = None,
+                       out_rank: torch.Tensor | None = None, out_max: torch.Tensor | None = None,
+                       out_sumexp: torch.Tensor | None = None, out_top_ids: torch.Tensor | None = None,
+                       out_top_logprobs: torch.Tensor | None = None, ctx_tokens: torch.Tensor | None = None,
+                       key: int = 0, gamma: float = 0.5, delta: float = 0.0, scheme: int = SCHEME_CONTEXT,
+                       V: int | None = None, vocab_offset: int = 0, stream=None) -> torch.Tensor | None:
+    """Log probability, entropy and rank of ``tokens`` (int32 ``[B]``, one per row of ``logits``), the rows'
+    softmax statistics and their ``n`` most probable alternatives (``out_top_ids`` int32 and
+    ``out_top_logprobs`` float32, both ``[B, n]``).  With ``delta`` the numbers are those of the watermarked
+    logits; ``logits`` itself is not changed.  A token outside ``[0, V)`` marks a padded row.  Outputs are
+    caller-allocated and may be left out; returns ``out_logprob``."""
+    B, V, ld = _logits_layout("logits", logits, V)
+    dev = logits.device
+    top = [t for t in (out_top_ids, out_top_logprobs) if t is not None]
+    if any(t.dim() != 2 or t.shape[0] != B or t.shape[1] != top[0].shape[1] for t in top):
+        raise ValueError("out_top_ids and out_top_logprobs must have shape [B, n]")
+    n = top[0].shape[1] if top else 0
+    f32, i32 = torch.float32, torch.int32
+    with _on(dev):
+        ctx, W = _watermark(ctx_tokens, B, delta, dev)
+        rc = lib().sbw_token_logprobs(
+            logits.data_ptr(), _dtype_code(logits), B, V, ld, vocab_offset, ctx, W, key, gamma, delta, scheme,
+            temperature, _expect("tokens", tokens, i32, B, dev), n, _expect("out_logprob", out_logprob, f32, B, dev),
+            _expect("out_entropy", out_entropy, f32, B, dev), _expect("out_rank", out_rank, i32, B, dev),
+            _expect("out_max", out_max, f32, B, dev), _expect("out_sumexp", out_sumexp, f32, B, dev),
+            _expect("out_top_ids", out_top_ids if n else None, i32, B * n, dev),
+            _expect("out_top_logprobs", out_top_logprobs if n else None, f32, B * n, dev), _stream(stream))
+    _check("sbw_token_logprobs", rc)
+    return out_logprob
+
+
+def sbw_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor | None, temperature: float,
+                                max: torch.Tensor, sumexp: torch.Tensor, grad_logits: torch.Tensor, *,
+                                grad_logprob: torch.Tensor | None = None, entropy: torch.Tensor | None = None,
+                                grad_entropy: torch.Tensor | None = None, ctx_tokens: torch.Tensor | None = None,
+                                key: int = 0, gamma: float = 0.5, delta: float = 0.0,
+                                scheme: int = SCHEME_CONTEXT, V: int | None = None, vocab_offset: int = 0,
+                                stream=None) -> torch.Tensor:
+    """Gradient of ``sum(grad_logprob * logprob + grad_entropy * entropy)`` with respect to ``logits`` into
+    ``grad_logits`` (same type, ``[B, >=V]``; may be ``logits`` itself), from the ``max``, ``sumexp`` and
+    ``entropy`` that :func:`sbw_token_logprobs` gave for the same arguments.  Returns ``grad_logits``."""
+    B, V, ld = _logits_layout("logits", logits, V)
+    gB, _, grad_ld = _logits_layout("grad_logits", grad_logits, V)
+    dev = logits.device
+    if gB != B or grad_logits.dtype != logits.dtype or grad_logits.device != dev:
+        raise ValueError("grad_logits must have logits' type, device and number of rows")
+    f32 = torch.float32
+    if max is None or sumexp is None:
+        raise TypeError("max and sumexp of the forward call are needed")
+    with _on(dev):
+        ctx, W = _watermark(ctx_tokens, B, delta, dev)
+        rc = lib().sbw_token_logprobs_backward(
+            logits.data_ptr(), _dtype_code(logits), B, V, ld, vocab_offset, ctx, W, key, gamma, delta, scheme,
+            temperature, _expect("tokens", tokens, torch.int32, B, dev), _expect("max", max, f32, B, dev),
+            _expect("sumexp", sumexp, f32, B, dev), _expect("entropy", entropy, f32, B, dev),
+            _expect("grad_logprob", grad_logprob, f32, B, dev), _expect("grad_entropy", grad_entropy, f32, B, dev),
+            grad_logits.data_ptr(), grad_ld, _stream(stream))
+    _check("sbw_token_logprobs_backward", rc)
+    return grad_logits
+
+
+def sbw_detect_weighted(tokens: torch.Tensor, weights: torch.Tensor, lengths: torch.Tensor, key: int, gamma: float,
+                        scheme: int, out_z: torch.Tensor, *, out_green: torch.Tensor | None = None,
+                        out_weight: torch.Tensor | None = None, out_weight2: torch.Tensor | None = None,
+                        offsets: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                        ctx_width: int = 1, stream=None) -> torch.Tensor:
+    """Batch detection with a float32 weight per token (entropies, or 0/1).  Outputs are float64 ``[N]``;
+    returns ``out_z``."""
+    N, total, dev = lengths.numel(), tokens.numel(), lengths.device
+    if not lengths.is_cuda:
+        raise ValueError("sbw_detect_weighted takes CUDA tensors")
+    if out_z is None:
+        raise TypeError("out_z is needed")
+    f64 = torch.float64
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise TypeError(f"workspace must be a contiguous tensor on {dev}")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with _on(dev):
+        rc = lib().sbw_detect_weighted(
+            _expect("tokens", tokens, torch.int32, total, dev), _expect("weights", weights, torch.float32, total, dev),
+            _expect("lengths", lengths, torch.int32, N, dev), _expect("offsets", offsets, torch.int64, N + 1, dev), N,
+            total, ctx_width, key, gamma, scheme, _expect("out_green", out_green, f64, N, dev),
+            _expect("out_weight", out_weight, f64, N, dev), _expect("out_weight2", out_weight2, f64, N, dev),
+            _expect("out_z", out_z, f64, N, dev), _ptr(workspace), ws_bytes, _stream(stream))
+    _check("sbw_detect_weighted", rc)
+    return out_z
 
 
 PROBE_KINDS = {"mulwide": (0, 1), "lop3": (1, 1), "iadd3": (2, 1), "imad": (3, 1), "philox": (4, 4),

@@ -9,6 +9,8 @@
 // without masks and only the last, ragged trip of a sequence is predicated.
 // Sequence starts come from a caller-supplied offsets array or from a two-kernel exclusive scan
 // of the lengths into the workspace.
+#include <cooperative_groups.h>
+
 #include "sbw_common.cuh"
 #include "sbw_hash.cuh"
 
@@ -400,6 +402,188 @@ int detect_impl(const int32_t *tokens, const int32_t *lengths, const int64_t *of
     }
     SBW_CUDA_TRY(err);
     return SBW_OK;
+}
+
+// ---- detection with a weight per token ----
+// The detector's trips, with three fp64 sums per lane in place of the ballot count: a weight is one
+// more coalesced load per token and the sums are a small part of the hash's work.  A lane sums its
+// positions in order and the lanes, warps and CTAs are joined in a fixed tree, so that equal calls
+// give equal bits.
+struct WeightSums {
+    double green, weight, weight2;
+    __device__ __forceinline__ void add(const WeightSums &o) {
+        green += o.green;
+        weight += o.weight;
+        weight2 += o.weight2;
+    }
+    __device__ __forceinline__ void join_warp() {
+        for (int d = 16; d > 0; d >>= 1) {
+            green += __shfl_xor_sync(0xffffffffu, green, d);
+            weight += __shfl_xor_sync(0xffffffffu, weight, d);
+            weight2 += __shfl_xor_sync(0xffffffffu, weight2, d);
+        }
+    }
+};
+
+struct WeightedArgs {
+    DetectArgs d;             // out_z is its output; the counts are not written
+    const float *weights;
+    double *out_green, *out_weight, *out_weight2;
+};
+
+template <int SCHEME, int WIDTH, bool TAIL, int ILP = kDetectIlp>
+__device__ __forceinline__ void weigh_trip(const WeightedArgs &a, const int32_t *tok, const float *weights, int base, int len,
+                                           int lane, WeightSums &sums) {
+    uint32_t v[ILP], x[ILP];
+    uint64_t r[ILP];
+    bool valid[ILP];
+    float w[ILP];
+#pragma unroll
+    for (int u = 0; u < ILP; ++u) {
+        const int t = base + u * 32 + lane;
+        w[u] = !TAIL || static_cast<unsigned>(t) < static_cast<unsigned>(len) ? weights[t] : 0.0f;
+    }
+    load_trip<SCHEME, WIDTH, TAIL, ILP>(a.d, tok, base, len, lane, v, r, valid);
+    philox_word0_n<ILP>(v, r, x, a.d.weyl);
+#pragma unroll
+    for (int u = 0; u < ILP; ++u) {
+        const double wd = static_cast<double>(w[u]);
+        if (valid[u] && x[u] <= a.d.thr_m1) sums.green += wd;
+        sums.weight += wd;
+        sums.weight2 = __fma_rn(wd, wd, sums.weight2);
+    }
+}
+
+__device__ __forceinline__ void write_weighted(const WeightedArgs &a, int64_t seq, const WeightSums &s) {
+    if (a.out_green) a.out_green[seq] = s.green;
+    if (a.out_weight) a.out_weight[seq] = s.weight;
+    if (a.out_weight2) a.out_weight2[seq] = s.weight2;
+    // Eq. 5 with S1 and S2 in T's places, every operation rounded separately
+    const double num = __dsub_rn(s.green, __dmul_rn(a.d.gamma, s.weight));
+    const double var = __dmul_rn(__dmul_rn(s.weight2, a.d.gamma), __dsub_rn(1.0, a.d.gamma));
+    a.d.out_z[seq] = s.weight2 == 0.0 ? 0.0 : __ddiv_rn(num, __dsqrt_rn(var));
+}
+
+template <int SCHEME, int WIDTH>
+__global__ void __launch_bounds__(kDetectThreads)
+weighted_kernel(const WeightedArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int64_t seq = static_cast<int64_t>(blockIdx.x) * (kDetectThreads / 32) + (threadIdx.x >> 5);
+    if (seq >= a.d.N) return;
+    const int64_t off = a.d.offsets[seq];
+    int64_t L = clamp_len(a.d.lengths[seq]);
+    if (off < 0 || off >= a.d.total_tokens) L = 0;
+    else if (off + L > a.d.total_tokens) L = a.d.total_tokens - off;
+    const int width = WIDTH > 0 ? WIDTH : a.d.W;
+    const int32_t *tok = a.d.tokens + off;
+    const float *weights = a.weights + off;
+    const int len = static_cast<int>(L);
+    constexpr int kTrip = 32 * kDetectIlp;
+    WeightSums sums = {0.0, 0.0, 0.0};
+    if (len > width) {
+        int base = width;
+        for (; len - base >= kTrip; base += kTrip) weigh_trip<SCHEME, WIDTH, false>(a, tok, weights, base, len, lane, sums);
+        if (len - base >= 64) {
+            weigh_trip<SCHEME, WIDTH, false, 2>(a, tok, weights, base, len, lane, sums);
+            base += 64;
+        }
+        if (len - base >= 32) {
+            weigh_trip<SCHEME, WIDTH, false, 1>(a, tok, weights, base, len, lane, sums);
+            base += 32;
+        }
+        if (base < len) weigh_trip<SCHEME, WIDTH, true, 1>(a, tok, weights, base, len, lane, sums);
+    }
+    sums.join_warp();
+    if (lane == 0) write_weighted(a, seq, sums);
+}
+
+// Few sequences: a CTA per sequence, and for few long ones a cluster of up to 8, its warps taking the
+// trips in turn; CTA 0 adds up the others' sums out of their shared memory.
+template <int SCHEME, int WIDTH>
+__global__ void __launch_bounds__(1024)
+weighted_wide_kernel(const WeightedArgs a) {
+    namespace cg = cooperative_groups;
+    __shared__ long long sh_before[32];
+    __shared__ WeightSums sh_warp[32];
+    __shared__ WeightSums sh_part;
+    const auto cluster = cg::this_cluster();
+    const int parts = static_cast<int>(cluster.num_blocks()), part = static_cast<int>(cluster.block_rank());
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+    const int64_t seq = blockIdx.x / parts;
+    int64_t off;
+    if (a.d.offsets) {
+        off = a.d.offsets[seq];
+    } else {
+        long long before = 0;
+        for (int64_t i = threadIdx.x; i < seq; i += blockDim.x) before += clamp_len(a.d.lengths[i]);
+        for (int d = 16; d > 0; d >>= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+        if (lane == 0) sh_before[warp] = before;
+        __syncthreads();
+        off = 0;
+        for (int w = 0; w < nwarps; ++w) off += sh_before[w];
+    }
+    int64_t L = clamp_len(a.d.lengths[seq]);
+    if (off < 0 || off >= a.d.total_tokens) L = 0;
+    else if (off + L > a.d.total_tokens) L = a.d.total_tokens - off;
+    const int width = WIDTH > 0 ? WIDTH : a.d.W;
+    const int32_t *tok = a.d.tokens + off;
+    const float *weights = a.weights + off;
+    const int len = static_cast<int>(L);
+    constexpr int kTrip = 32 * kDetectIlp;
+    const int full = len > width ? (len - width) / kTrip : 0;         // unmasked trips
+    const int tail_base = width + full * kTrip;
+    const int walkers = parts * nwarps, me = part * nwarps + warp;
+    WeightSums sums = {0.0, 0.0, 0.0};
+    for (int i = me; i < full; i += walkers) weigh_trip<SCHEME, WIDTH, false>(a, tok, weights, width + i * kTrip, len, lane, sums);
+    if (tail_base < len && me == full % walkers) weigh_trip<SCHEME, WIDTH, true>(a, tok, weights, tail_base, len, lane, sums);
+    sums.join_warp();
+    if (lane == 0) sh_warp[warp] = sums;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        WeightSums total = sh_warp[0];
+        for (int w = 1; w < nwarps; ++w) total.add(sh_warp[w]);
+        sh_part = total;
+    }
+    cluster.sync();
+    if (part == 0 && threadIdx.x == 0) {
+        WeightSums total = sh_part;
+        for (int r = 1; r < parts; ++r) total.add(*cluster.map_shared_rank(&sh_part, r));
+        write_weighted(a, seq, total);
+    }
+    cluster.sync();                                                   // the sums have been read
+}
+
+template <int SCHEME>
+cudaError_t launch_weighted(const WeightedArgs &a, int sm_count, cudaStream_t s) {
+    if (const int wide = wide_threads(a.d.N, sm_count)) {
+        // a cluster per sequence while sequences are long enough to keep its CTAs' warps in trips
+        const int64_t mean = a.d.total_tokens / a.d.N;
+        int parts = 1;
+        while (parts < 8 && a.d.N * parts * 2 <= sm_count && mean > static_cast<int64_t>(parts) * 32 * 32 * kDetectIlp) parts *= 2;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(a.d.N * parts));
+        cfg.blockDim = dim3(static_cast<unsigned>(wide));
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        switch (a.d.W) {
+            case 1: return cudaLaunchKernelEx(&cfg, weighted_wide_kernel<SCHEME, 1>, a);
+            case 4: return cudaLaunchKernelEx(&cfg, weighted_wide_kernel<SCHEME, 4>, a);
+            default: return cudaLaunchKernelEx(&cfg, weighted_wide_kernel<SCHEME, 0>, a);
+        }
+    }
+    const unsigned grid = static_cast<unsigned>((a.d.N + kDetectThreads / 32 - 1) / (kDetectThreads / 32));
+    switch (a.d.W) {
+        case 1: weighted_kernel<SCHEME, 1><<<grid, kDetectThreads, 0, s>>>(a); break;
+        case 4: weighted_kernel<SCHEME, 4><<<grid, kDetectThreads, 0, s>>>(a); break;
+        default: weighted_kernel<SCHEME, 0><<<grid, kDetectThreads, 0, s>>>(a); break;
+    }
+    return cudaGetLastError();
 }
 
 // ---- windowed detection on the stored green bits ----
@@ -815,5 +999,49 @@ extern "C" int sbw_detect_unique(const int32_t *tokens, const int32_t *lengths, 
     const unsigned grid = static_cast<unsigned>(blocks < resident ? blocks : resident);
     SBW_CUDA_TRY(scheme == SBW_SCHEME_CONTEXT ? launch_detect_unique<SBW_SCHEME_CONTEXT>(a, tables, next, grid, s)
                                               : launch_detect_unique<SBW_SCHEME_SELFSALT>(a, tables, next, grid, s));
+    return SBW_OK;
+}
+
+extern "C" int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32_t *lengths,
+                                   const int64_t *offsets, int64_t N, int64_t total_tokens, int ctx_width,
+                                   uint64_t key, double gamma, int scheme, double *out_green, double *out_weight,
+                                   double *out_weight2, double *out_z, void *workspace, size_t workspace_bytes,
+                                   void *stream) {
+    using namespace sbw;
+    if (!valid_common(SBW_DTYPE_F32, ctx_width, gamma, scheme)) return SBW_ERR_INVALID_ARG;
+    if (N < 0 || total_tokens < 0) return SBW_ERR_INVALID_ARG;
+    if (N == 0) return SBW_OK;
+    if (N > (int64_t(1) << 31) * (kDetectThreads / 32) - 1) return SBW_ERR_UNSUPPORTED;
+    if (!lengths || !out_z) return SBW_ERR_INVALID_ARG;
+    if ((!tokens || !weights) && total_tokens > 0) return SBW_ERR_INVALID_ARG;
+    if (!offsets && (!workspace || workspace_bytes < sbw_detect_workspace_bytes(N) ||
+                     reinterpret_cast<uintptr_t>(workspace) % 256 != 0))
+        return SBW_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    WeightedArgs a = {};
+    a.d.tokens = tokens;
+    a.d.lengths = lengths;
+    a.d.offsets = offsets;
+    a.d.N = N;
+    a.d.total_tokens = total_tokens;
+    a.d.W = ctx_width;
+    a.d.key = key;
+    a.d.thr_m1 = threshold_minus_one(gamma);
+    a.d.gamma = gamma;
+    a.d.out_z = out_z;
+    a.d.weyl = make_weyl();
+    a.weights = weights;
+    a.out_green = out_green;
+    a.out_weight = out_weight;
+    a.out_weight2 = out_weight2;
+    DeviceInfo di;
+    if (int rc = current_device_info(&di)) return rc;
+    if (!offsets && wide_threads(N, di.sm_count) == 0) {
+        int64_t *scanned = nullptr;
+        if (int rc = scan_lengths(lengths, N, workspace, &scanned, s)) return rc;
+        a.d.offsets = scanned;
+    }
+    SBW_CUDA_TRY(scheme == SBW_SCHEME_CONTEXT ? launch_weighted<SBW_SCHEME_CONTEXT>(a, di.sm_count, s)
+                                              : launch_weighted<SBW_SCHEME_SELFSALT>(a, di.sm_count, s));
     return SBW_OK;
 }

@@ -32,6 +32,7 @@
 #include "sbw_common.cuh"
 #include "sbw_hash.cuh"
 #include "sbw_gumbel.cuh"
+#include "sbw_rowbias.cuh"
 
 namespace sbw {
 namespace {
@@ -95,25 +96,11 @@ __device__ __forceinline__ float decode_score(unsigned c) {
     return __uint_as_float((c & 0x80000000u) ? (c & 0x7fffffffu) : ~c);
 }
 
-__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
 __device__ __forceinline__ float ex2_approx(float x) {
     float y;
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// The same with results below 2^-126 flushed to zero (one instruction instead of a scaled
-// sequence): for terms of a sum whose largest term is 1.
-__device__ __forceinline__ float ex2_approx_ftz(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // exp2(d * c) for d <= 0 with c = c_hi + c_lo: returns e = exp2(round(d c_hi)) and the residual
 // `lo` such that the true value is e * 2^lo ~ e * (1 + lo ln 2).
 __device__ __forceinline__ float exp2_split(float d, float c_hi, float c_lo, float &lo) {
@@ -154,55 +141,6 @@ struct Best {
 };
 __device__ __forceinline__ bool better(float s1, int id1, float s2, int id2) {
     return s1 > s2 || (s1 == s2 && id1 < id2);
-}
-
-template <int SCHEME>
-struct RowSeedS;
-template <>
-struct RowSeedS<SBW_SCHEME_CONTEXT> {
-    RowKeys rk;
-    __device__ __forceinline__ void init(uint64_t key, const int32_t *ctx, int W) {
-        rk = make_row_keys(seed_context(key, ctx, W));
-    }
-    __device__ __forceinline__ uint32_t word0(uint32_t v, uint64_t, const Weyl) const {
-        return philox_word0(v, rk);
-    }
-    template <int N>
-    __device__ __forceinline__ void word0_n(uint32_t vg, uint64_t, const Weyl, uint32_t (&x)[N]) const {
-        philox_word0_n<N>(vg, rk, x);
-    }
-};
-template <>
-struct RowSeedS<SBW_SCHEME_SELFSALT> {
-    uint32_t jmin;
-    __device__ __forceinline__ void init(uint64_t, const int32_t *ctx, int W) { jmin = jenkins_min(ctx, W); }
-    __device__ __forceinline__ uint32_t word0(uint32_t v, uint64_t key, const Weyl w) const {
-        return philox_word0(v, seed_selfsalt(key, jmin, v), w);
-    }
-    template <int N>
-    __device__ __forceinline__ void word0_n(uint32_t vg, uint64_t key, const Weyl w, uint32_t (&x)[N]) const {
-        uint32_t v[N];
-        uint64_t r[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = vg + i;
-            r[i] = seed_selfsalt(key, jmin, v[i]);
-        }
-        philox_word0_n<N>(v, r, x, w);
-    }
-};
-
-// Biased logit of one element, widened to fp32 (Eq. 2 in the logits' own precision).
-template <int DTYPE>
-__device__ __forceinline__ float biased(uint32_t raw, bool green, float delta) {
-    if constexpr (DTYPE == SBW_DTYPE_F32) {
-        const float x = __uint_as_float(raw);
-        return green ? __fadd_rn(x, delta) : x;
-    } else {
-        const float x = __uint_as_float(raw << 16);
-        // fp32 sum of two bf16 values, rounded once more to bf16 = correctly rounded bf16 sum
-        return green ? __bfloat162float(__float2bfloat16_rn(__fadd_rn(x, delta))) : x;
-    }
 }
 
 // Final per-row merge of `n` partials by one warp.  Two passes over the partials (they sit in
