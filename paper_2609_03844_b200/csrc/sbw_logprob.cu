@@ -12,8 +12,10 @@
 //     dl_v = 1/tau [ g (1[v = t] - p_v) - h p_v (ln p_v + H) ].
 #include <cooperative_groups.h>
 
+#include <atomic>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "sbw_codes.cuh"
 #include "sbw_common.cuh"
@@ -22,14 +24,18 @@
 namespace sbw {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
-constexpr int kGroups = kThreads / 4;   // maxima of disjoint column sets that bound the alternatives from below
-constexpr int kCap = 2048;              // candidate list entries
+// CTA size.  Without the hash three CTAs of 256 threads per SM (80 registers).  With it (128 registers) four of
+// 128: the same 16 warps as the other hashing kernels, in smaller pieces, so that a call's CTAs share the
+// SMs out more evenly.
+__host__ __device__ constexpr int threads_of(int scheme) { return scheme < 0 ? 256 : 128; }
+__host__ __device__ constexpr int ctas_per_sm(int scheme) { return scheme < 0 ? 3 : 4; }
+constexpr int kCap = 1280;              // candidate list entries
+constexpr int kKeep = 256;              // candidates left after the last cut, for the fast ranking
 constexpr int kMaxTop = SBW_MAX_TOP_LOGPROBS;
-constexpr int kMaxCluster = 8;
+// CTAs per row at most
+__host__ __device__ constexpr int max_parts(int scheme, bool top) { return scheme < 0 && top ? 8 : 16; }
 constexpr float kFar = -300.0f;         // exponents below this give 2^x = 0; keeps 0 * inf out of the sums
-static_assert(kCap >= 32 * kMaxTop, "a row with fewer groups than alternatives must fit the list");
+static_assert(kCap >= 16 * kMaxTop + 16, "a share with vectors for fewer groups than alternatives must fit the list");
 
 struct LogprobArgs {
     const void *logits;
@@ -38,7 +44,7 @@ struct LogprobArgs {
     int W;
     uint32_t vocab_offset;
     BiasParams bias;
-    double tau;
+    double inv_tau;
     float c;               // log2(e) / tau
     const int32_t *tokens; // nullable
     int top_n;
@@ -49,30 +55,6 @@ struct LogprobArgs {
     float *out_top_logprobs;
 };
 
-// ---- two fp32 operations per instruction ----
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t p, float &lo, float &hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
 // max that keeps a NaN (fmaxf drops it): a NaN logit has to reach the sums
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
@@ -105,18 +87,25 @@ __device__ __forceinline__ float composite_value(uint64_t e) {
     return __uint_as_float(order_decode(static_cast<uint32_t>(e >> 32)));
 }
 
+// Running sums of a set of columns.  Exponents are taken as l c - ref in one fused operation, so ref,
+// a rounded m c, is itself the reference: nothing depends on how m c was rounded.
 struct Stats {
-    float m, z, s;    // reference (a maximum, at least -FLT_MAX), sum, first moment in log2 units
+    float ref, z, s;  // reference (log2 units), sum of 2^(l c - ref), of the same times (l c - ref)
+    float top;        // largest value, -inf if none
     uint32_t above;   // columns that rank before the token
-    // the same sums with reference `to` >= m
-    __device__ __forceinline__ void move(float to, float c) {
-        const float d = fmaxf((m - to) * c, kFar);
+    // the same sums with reference `to` >= ref
+    __device__ __forceinline__ void move(float to) {
+        const float d = fmaxf(ref - to, kFar);
         const float f = ex2_approx_ftz(d);
         s = f * fmaf(d, z, s);
         z *= f;
-        m = to;
+        ref = to;
     }
 };
+// Columns below m - 300 / c count as that (2^-300 = 0), a thread that has met no ordinary value has the
+// reference of -2^100, and rows whose largest value is not within +-2^90 are summed again by
+// sum_plainly: with temperatures within 1e-6 .. 1e6 nothing overflows and no 0 * inf arises.
+constexpr float kNoValue = -0x1p100f, kOrdinary = 0x1p90f;
 
 // Largest value of a vector, NaN dropped.
 template <int DTYPE>
@@ -130,6 +119,23 @@ __device__ __forceinline__ float vector_max(const uint4 &w) {
     }
 }
 
+// The same over n vectors (bf16: two halves at a time to the end).
+template <int DTYPE, int N>
+__device__ __forceinline__ float largest_of(const uint4 (&w)[N]) {
+    if constexpr (DTYPE == SBW_DTYPE_F32) {
+        float m = vector_max<DTYPE>(w[0]);
+#pragma unroll
+        for (int u = 1; u < N; ++u) m = fmaxf(m, vector_max<DTYPE>(w[u]));
+        return m;
+    } else {
+        const __nv_bfloat162 *e = reinterpret_cast<const __nv_bfloat162 *>(w);
+        __nv_bfloat162 m = e[0];
+#pragma unroll
+        for (int i = 1; i < 4 * N; ++i) m = __hmax2(m, e[i]);
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+}
+
 template <int DTYPE>
 __device__ __forceinline__ float element(const uint4 &w, int i) {
     const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
@@ -138,14 +144,25 @@ __device__ __forceinline__ float element(const uint4 &w, int i) {
 }
 
 __device__ __forceinline__ uint4 load_vector(const uint4 *p) {
-    uint4 r;   // read once: no need to keep it in L1
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    uint4 r;   // read once, not kept in L1; no .nc: the kernel may write over what it has read
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     return r;
 }
 
-__device__ __forceinline__ uint4 load_vector_rw(const uint4 *p) {
-    uint4 r;   // the same where the kernel may write over what it has read
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+// The next value below x in the logits' type (x no NaN and not -inf).
+template <int DTYPE>
+__device__ __forceinline__ float value_below(float x) {
+    constexpr uint32_t ulp = DTYPE == SBW_DTYPE_F32 ? 1u : 0x10000u;
+    const uint32_t b = __float_as_uint(x);
+    return __uint_as_float((b << 1) == 0 ? 0x80000000u + ulp : (b & 0x80000000u) ? b + ulp : b - ulp);
+}
+__device__ __forceinline__ uint32_t both_halves(float bf16_value) {
+    const uint32_t b = __float_as_uint(bf16_value);
+    return (b & 0xffff0000u) | (b >> 16);
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 
@@ -165,23 +182,50 @@ struct Columns {
     }
 };
 
+// The sums of columns [lo, hi) for rows with values of any size, by the whole CTA: the largest value
+// first, then differences.  ref is 0 here and z relative to `top`.
+template <int DTYPE, int SCHEME>
+__device__ __noinline__ Stats sum_plainly(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, float top, Stats *scratch) {
+    const Columns<DTYPE, SCHEME> x(a, row);
+    Stats st = {0.0f, 0.0f, 0.0f, top, 0u};
+    for (uint32_t col = lo + threadIdx.x; col < hi; col += blockDim.x) {
+        const float d = max_nan((x[col] - top) * a.c, kFar);
+        const float e = ex2_approx_ftz(d);
+        st.z += e;
+        st.s = fmaf(e, d, st.s);
+    }
+    for (int d = 16; d > 0; d >>= 1) {
+        st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
+        st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = st;
+    __syncthreads();
+    st.z = st.s = 0.0f;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
+        st.z += scratch[w].z;
+        st.s += scratch[w].s;
+    }
+    return st;
+}
+
 // Columns that rank before column t when its value is -inf (or NaN, which counts as that).
 template <int DTYPE, int SCHEME>
 __device__ __noinline__ uint32_t count_above_nothing(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, uint32_t t) {
     const Columns<DTYPE, SCHEME> x(a, row);
     uint32_t n = 0;
-    for (uint32_t col = lo + threadIdx.x; col < hi; col += kThreads) n += (x[col] > -INFINITY || col < t) ? 1u : 0u;
+    for (uint32_t col = lo + threadIdx.x; col < hi; col += blockDim.x) n += (x[col] > -INFINITY || col < t) ? 1u : 0u;
     return n;
 }
 
-// Candidates strictly above `floor`.
+// Candidates from `floor` on, or strictly above it.
 template <int DTYPE, int SCHEME>
-__device__ __noinline__ void gather_above(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, float floor, uint64_t *list,
-                                          unsigned *count) {
+__device__ __noinline__ void gather_again(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, float floor, bool strict,
+                                          uint64_t *list, unsigned *count) {
     const Columns<DTYPE, SCHEME> x(a, row);
-    for (uint32_t col = lo + threadIdx.x; col < hi; col += kThreads) {
+    for (uint32_t col = lo + threadIdx.x; col < hi; col += blockDim.x) {
         const float v = x[col];
-        if (v > floor) {
+        if (v > floor || (!strict && v == floor)) {
             const unsigned pos = atomicAdd(count, 1u);
             if (pos < static_cast<unsigned>(kCap)) list[pos] = composite(v, col);
         }
@@ -213,7 +257,7 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
     uint64_t last = ~0ull;
     for (unsigned r = 0; r < need; ++r) {
         uint64_t best = 0;
-        for (uint32_t col = lo + threadIdx.x; col < hi; col += kThreads) {
+        for (uint32_t col = lo + threadIdx.x; col < hi; col += blockDim.x) {
             const uint64_t e = composite(x[col], col);
             if (e < last && e > best) best = e;
         }
@@ -223,307 +267,508 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
         }
         if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = best;
         __syncthreads();
-        for (int w = 0; w < kWarps; ++w) best = scratch[w] > best ? scratch[w] : best;
+        for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) best = scratch[w] > best ? scratch[w] : best;
         if (threadIdx.x == 0) list[r] = best;
         last = best;
         __syncthreads();
     }
 }
 
-// One CTA per row for large batches, a cluster of up to 8 CTAs per row for small ones: each CTA
-// takes a share of the row's vectors, and CTA 0 merges the others' sums and alternatives out of
-// their shared memory.  No workspace, no atomics outside a CTA, one launch.
+// ---- the row pass ----
+// Every thread copies its own vectors into its own slots of shared memory, groups of a few vectors
+// some groups ahead (cp.async: no register waits for the data, no barrier, and a thread waits for
+// nothing but its own copies), across row boundaries too, so that the loads go on while a row is finished.
+template <int SCHEME, bool TOP>
+struct Ring {
+    static constexpr int kGroup = SCHEME == kSchemeNone ? 4 : 2;             // vectors of a group; a trip takes one group
+    static constexpr int kStages = SCHEME == kSchemeNone && TOP ? 2 : 3;
+    static constexpr int kThreads = threads_of(SCHEME);
+    static constexpr int kGroupBytes = kGroup * kThreads * 16;
+    static constexpr int kBytes = kGroupBytes * kStages;
+};
+__device__ __forceinline__ void copy_async(uint32_t smem, const uint4 *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(src));
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N));
+}
+__device__ __forceinline__ uint4 load_shared(uint32_t smem) {
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem));
+    return r;
+}
+
+// The share of CTA `part` of `parts` in a row.
+template <int DTYPE>
+struct Share {
+    const uint4 *vectors;
+    uint32_t head, v_lo, v_hi;
+    __device__ __forceinline__ Share() : vectors(nullptr), head(0), v_lo(0), v_hi(0) {}
+    __device__ __forceinline__ Share(const LogprobArgs &a, int64_t row, unsigned part, unsigned parts) {
+        const char *row_ptr = static_cast<const char *>(a.logits) + row * a.ld * RowLayout<DTYPE>::ESIZE;
+        const RowLayout<DTYPE> layout(row_ptr, static_cast<uint32_t>(a.V));
+        head = layout.head;
+        vectors = reinterpret_cast<const uint4 *>(row_ptr + static_cast<size_t>(head) * RowLayout<DTYPE>::ESIZE);
+        v_lo = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * part / parts);
+        v_hi = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * (part + 1) / parts);
+    }
+    template <uint32_t PER_TRIP>
+    __device__ __forceinline__ uint32_t trips() const {
+        return max(1u, (v_hi - v_lo + PER_TRIP - 1) / PER_TRIP);
+    }
+};
+
+// The largest value that at least n of the group maxima reach, by the first `groups` threads; needs
+// barriers on both sides.
+__device__ __forceinline__ void bound_below(const float *group, int groups, int n, unsigned *out) {
+    const int i = threadIdx.x;
+    if (i >= groups) return;
+    const float mine = group[i];
+    int reach = 0;
+    const float4 *g4 = reinterpret_cast<const float4 *>(group);
+#pragma unroll 8
+    for (int o = 0; o < groups / 4; ++o) {
+        const float4 g = g4[o];
+        reach += (g.x >= mine ? 1 : 0) + (g.y >= mine ? 1 : 0) + (g.z >= mine ? 1 : 0) + (g.w >= mine ? 1 : 0);
+    }
+    const unsigned best = __reduce_max_sync(0xffffffffu, reach >= n ? value_code(mine) : 0u);
+    if ((i & 31) == 0) atomicMax(out, best);
+}
+
+// Entries of a 16-byte aligned list that are larger than `mine`.
+__device__ __forceinline__ unsigned count_larger(const uint64_t *list, unsigned n, uint64_t mine) {
+    unsigned r0 = 0, r1 = 0;
+    const ulonglong2 *pairs = reinterpret_cast<const ulonglong2 *>(list);
+#pragma unroll 8
+    for (unsigned o = 0; o < n / 2; ++o) {
+        const ulonglong2 q = pairs[o];
+        r0 += q.x > mine ? 1u : 0u;
+        r1 += q.y > mine ? 1u : 0u;
+    }
+    if (n & 1u) r0 += list[n - 1] > mine ? 1u : 0u;
+    return r0 + r1;
+}
+
+// One CTA per row for large batches (the CTAs go on from row to row), a cluster of up to 16 CTAs per
+// row for small ones: each CTA takes a share of the row's vectors and leaves its sums and
+// alternatives in the shared memory of CTA 0, which merges them.  No workspace, no atomics outside a CTA,
+// one launch.
 template <int DTYPE, int SCHEME, bool TOP>
-__global__ void __launch_bounds__(kThreads, SCHEME == kSchemeNone ? 2 : 1)
+__global__ void __launch_bounds__(threads_of(SCHEME), ctas_per_sm(SCHEME))
 logprob_kernel(const __grid_constant__ LogprobArgs a) {
     namespace cg = cooperative_groups;
     using Layout = RowLayout<DTYPE>;
     constexpr int VEC = Layout::VEC;
-    constexpr int U = SCHEME == kSchemeNone ? 4 : 2;    // vectors in flight per thread
-    __shared__ Stats sh_warp[kWarps];
-    __shared__ Stats sh_part;
-    __shared__ float sh_group[TOP ? kGroups : 1];
-    __shared__ float sh_floor;
-    __shared__ unsigned sh_count;
-    __shared__ uint64_t sh_scratch[kWarps];
-    __shared__ uint64_t sh_list[TOP ? kCap : 1];
-    __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];      // this part's alternatives, best first, 0 = none
-    __shared__ uint64_t sh_all[TOP ? kMaxTop * kMaxCluster : 1];
+    using R = Ring<SCHEME, TOP>;
+    constexpr int U = R::kGroup, kThreads = R::kThreads, kWarps = kThreads / 32;
+    extern __shared__ __align__(16) unsigned char sh_ring[];
+    __shared__ Stats sh_warp[2][max_parts(SCHEME, TOP) * kWarps];            // of two rows in turn
+    __shared__ Stats sh_scratch[kWarps];
+    __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
+    __shared__ unsigned sh_floor, sh_count, sh_kept;
+    __shared__ __align__(16) uint64_t sh_list[TOP ? kCap : 1];
+    __shared__ __align__(16) uint64_t sh_keep[TOP ? kKeep : kWarps];
+    __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];               // this part's alternatives, best first, 0 = none
+    __shared__ __align__(16) uint64_t sh_all[TOP ? kMaxTop * max_parts(SCHEME, TOP) : 1];  // every part's, in CTA 0
 
     const auto cluster = cg::this_cluster();
     const unsigned parts = cluster.num_blocks(), part = cluster.block_rank();
     const uint32_t V = static_cast<uint32_t>(a.V);
     const float c = a.c;
-    const uint64_t c2 = pack2(c, c);
     const unsigned tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t step = gridDim.x / parts;
+    const int groups = a.top_n <= 32 ? 64 : 128;                 // sets of columns whose maxima bound the alternatives
+    if (parts > 1) cluster.barrier_arrive();                     // waited for before another CTA's memory is written
 
-    for (int64_t row = blockIdx.x / parts; row < a.B; row += gridDim.x / parts) {
-        const char *row_ptr = static_cast<const char *>(a.logits) + row * a.ld * Layout::ESIZE;
-        const uint32_t t = a.tokens ? static_cast<uint32_t>(a.tokens[row]) : 0u;
-        if (a.tokens && t >= V) {                        // a padded row: every CTA of the cluster skips it
+    if (TOP && tid == 0) sh_count = sh_kept = sh_floor = 0;
+    const float far = 300.0f / c;
+    int buf = 0;
+
+    // The first row from r on that is not padded; what a padded row gets is written on the way.
+    auto next_real = [&](int64_t r, uint32_t token) -> int64_t {
+        while (r < a.B && a.tokens && token >= V) {
             if (part == 0) {
                 if (tid == 0) {
-                    if (a.out_logprob) a.out_logprob[row] = 0.0f;
-                    if (a.out_entropy) a.out_entropy[row] = 0.0f;
-                    if (a.out_rank) a.out_rank[row] = 0;
-                    if (a.out_max) a.out_max[row] = 0.0f;
-                    if (a.out_sumexp) a.out_sumexp[row] = 0.0f;
+                    if (a.out_logprob) a.out_logprob[r] = 0.0f;
+                    if (a.out_entropy) a.out_entropy[r] = 0.0f;
+                    if (a.out_rank) a.out_rank[r] = 0;
+                    if (a.out_max) a.out_max[r] = 0.0f;
+                    if (a.out_sumexp) a.out_sumexp[r] = 0.0f;
                 }
                 for (unsigned i = tid; TOP && i < static_cast<unsigned>(a.top_n); i += kThreads) {
-                    if (a.out_top_ids) a.out_top_ids[row * a.top_n + i] = -1;
-                    if (a.out_top_logprobs) a.out_top_logprobs[row * a.top_n + i] = -INFINITY;
+                    if (a.out_top_ids) a.out_top_ids[r * a.top_n + i] = -1;
+                    if (a.out_top_logprobs) a.out_top_logprobs[r * a.top_n + i] = -INFINITY;
                 }
             }
-            continue;
+            r += step;
+            if (r < a.B) token = static_cast<uint32_t>(a.tokens[r]);
         }
+        return r;
+    };
+    auto token_of = [&](int64_t r) -> uint32_t { return a.tokens && r < a.B ? static_cast<uint32_t>(a.tokens[r]) : 0u; };
+
+    // The copying side: the next group's first vector of this thread, how many vectors the share has from
+    // there on, and how many groups.
+    const uint32_t slots = static_cast<uint32_t>(__cvta_generic_to_shared(sh_ring)) + tid * 16;
+    int64_t src_row = static_cast<int64_t>(blockIdx.x / parts) - step;
+    const uint4 *src = nullptr;
+    int src_left = 0;
+    uint32_t src_groups = 0, src_slot = 0;
+    auto next_slot = [](uint32_t s) { return s + R::kGroupBytes == R::kBytes ? 0u : s + R::kGroupBytes; };
+    auto copy_checked = [&]() {
+        if (src_groups == 0) {                                   // on to the next row that is not padded
+            do src_row += step;
+            while (parts == 1 && src_row < a.B && a.tokens && static_cast<uint32_t>(a.tokens[src_row]) >= V);
+            src_left = 0;
+            src_groups = 0xffffffffu;                            // after the last row: empty groups
+            if (src_row < a.B) {
+                const Share<DTYPE> share(a, src_row, part, parts);
+                src = share.vectors + share.v_lo + tid;
+                src_left = static_cast<int>(share.v_hi - share.v_lo - tid);
+                src_groups = share.template trips<U * kThreads>();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (src_left > u * kThreads) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+        copy_commit();
+        src += U * kThreads;
+        src_left -= U * kThreads;
+        --src_groups;
+        src_slot = next_slot(src_slot);
+    };
+#pragma unroll
+    for (int i = 0; i < R::kStages - 1; ++i) copy_checked();
+    uint32_t slot = 0;
+
+    int64_t row = blockIdx.x / parts;
+    uint32_t t = token_of(row);
+    row = next_real(row, t);
+    if (row >= a.B && parts > 1) cluster.barrier_wait();
+
+    while (row < a.B) {
+        const char *row_ptr = static_cast<const char *>(a.logits) + row * a.ld * Layout::ESIZE;
+        t = token_of(row);
+        const uint32_t token_ahead = token_of(row + step);
         RowSeedS<SCHEME> rs;
         rs.init(a.bias.key, a.ctx + row * a.W, a.W);
-        const Layout layout(row_ptr, V);
-        const uint4 *vectors = reinterpret_cast<const uint4 *>(row_ptr + static_cast<size_t>(layout.head) * Layout::ESIZE);
-        const uint32_t v_lo = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * part / parts);
-        const uint32_t v_hi = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * (part + 1) / parts);
-        // this part's columns: its vectors, and the ragged ends with the first and the last part
-        const uint32_t c_lo = part == 0 ? 0u : layout.head + v_lo * VEC;
-        const uint32_t c_hi = part + 1 == parts ? V : layout.head + v_hi * VEC;
+        const Share<DTYPE> share(a, row, part, parts);
+        const uint32_t nvec = (V - share.head) / VEC;
+        // this part's columns: its vectors, the head with the first part, the tail with the last
+        const uint32_t c_lo = part == 0 ? 0u : share.head + share.v_lo * VEC;
+        const uint32_t c_hi = part + 1 == parts ? V : share.head + share.v_hi * VEC;
 
-        // the token's own value, and the values its rank is counted against: strictly greater ones
-        // from its column on, before it also equal ones (greater than the next value below)
+        // the ragged ends: at most one column per thread
+        float xe = -INFINITY;
+        uint32_t ce = V;
+        if (part == 0 && tid < share.head) ce = tid;
+        else if (part + 1 == parts && tid >= 32 && tid - 32 < V - share.head - nvec * VEC) ce = share.head + nvec * VEC + tid - 32;
+        if (ce < V) xe = biased_at<DTYPE, SCHEME>(row_ptr, ce, rs, a.vocab_offset + ce, a.bias);
+
+        // the token's own value; its rank counts the greater ones, and the equal ones before it
         const bool ranked = a.tokens != nullptr && a.out_rank != nullptr;
         float xt = INFINITY;
         if (a.tokens) xt = biased_at<DTYPE, SCHEME>(row_ptr, t, rs, a.vocab_offset + t, a.bias);
         const bool t_nothing = ranked && !(xt > -INFINITY);
         const float bar = ranked && !t_nothing ? xt : INFINITY;
 
-        Stats st = {-FLT_MAX, 0.0f, 0.0f, 0u};
-        uint64_t z2 = 0, s2 = 0;                         // pairs of partial sums
-        float floor = INFINITY;                          // alternatives have at least this value
+        const float below = value_below<DTYPE>(bar);             // equal ones before the token are greater than that
+        const uint32_t bar2 = both_halves(bar), below2 = both_halves(below);
+        Stats st = {kNoValue * c, 0.0f, 0.0f, -INFINITY, 0u};
+        float least = kNoValue;                                  // values below count as this
+        [[maybe_unused]] uint32_t least2 = both_halves(kNoValue);
+        float count = 0.0f;                                      // columns that rank before the token
+        float floor = INFINITY;                                  // alternatives have at least this value
 
-        auto fold = [&]() {                              // z2, s2 into st
-            float lo, hi;
-            unpack2(z2, lo, hi);
-            st.z += lo + hi;
-            unpack2(s2, lo, hi);
-            st.s += lo + hi;
-            z2 = s2 = 0;
-        };
         auto push = [&](float x, uint32_t col) {
             if (x >= floor && x > -INFINITY) {
                 const unsigned pos = atomicAdd(&sh_count, 1u);
                 if (pos < static_cast<unsigned>(kCap)) sh_list[pos] = composite(x, col);
             }
         };
-
-        // ragged ends: at most one column per thread
-        float xe = -INFINITY;
-        uint32_t ce = V;
-        {
-            const uint32_t first_tail = layout.head + layout.nvec * VEC;
-            if (part == 0 && tid < layout.head) ce = tid;
-            else if (part + 1 == parts && tid >= 32 && tid - 32 < V - first_tail) ce = first_tail + tid - 32;
-            if (ce < V) {
-                xe = biased_at<DTYPE, SCHEME>(row_ptr, ce, rs, a.vocab_offset + ce, a.bias);
-                if (xe > st.m) st.m = xe;
-                const float x = max_nan((xe - st.m) * c, kFar);
-                const float e = ex2_approx_ftz(x);
-                st.z += e;
-                st.s = fmaf(e, x, st.s);
-                if (xe > bar || (xe == bar && ce < t)) st.above += 1u;
+        auto new_floor = [&](float with) {                       // two barriers
+            const int members = kThreads / groups;               // 4, 2 or 1 threads
+            float g = with;
+            if (members > 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
+            if (members > 2) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+            if ((tid & (members - 1)) == 0) sh_group[tid / members] = g;
+            __syncthreads();
+            bound_below(sh_group, groups, a.top_n, &sh_floor);
+            __syncthreads();
+            floor = __uint_as_float(order_decode(sh_floor));     // at least n columns reach it; -inf: perhaps not
+        };
+        float2 z2 = {0.0f, 0.0f}, s2 = {0.0f, 0.0f};             // partial sums of the trip
+        auto fold = [&]() {
+            st.z += z2.x + z2.y;
+            st.s += s2.x + s2.y;
+            z2 = s2 = make_float2(0.0f, 0.0f);
+        };
+        auto raise = [&](float m) {                              // a new largest value
+            fold();
+            st.top = m;
+            if (m > kNoValue) {
+                st.move(m * c);
+                least = __fsub_rd(m, far);
+                least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
             }
-        }
-
-        const uint32_t n_vec = v_hi - v_lo;
-        const uint32_t trips = max(1u, (n_vec + U * kThreads - 1) / (U * kThreads));
-        for (uint32_t trip = 0; trip < trips; ++trip) {
-            const uint32_t j0 = v_lo + trip * (U * kThreads) + tid;
+        };
+        // two columns in each operation
+        auto add_pair = [&](float l0, float l1) {
+            const float2 x = __ffma2_rn(make_float2(l0, l1), make_float2(c, c), make_float2(-st.ref, -st.ref));
+            const float2 e = make_float2(ex2_approx_ftz(x.x), ex2_approx_ftz(x.y));
+            z2 = __fadd2_rn(z2, e);
+            s2 = __ffma2_rn(e, x, s2);
+        };
+        uint32_t trip = 0;
+        uint32_t j0 = share.v_lo + tid;                          // this trip's first vector
+        auto trip_body = [&](const auto inside_tag) {
+            constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
             uint4 w[U];
+            copy_wait<R::kStages - 2>();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint32_t j = j0 + u * kThreads;
-                const uint32_t none = DTYPE == SBW_DTYPE_F32 ? 0xff800000u : 0xff80ff80u;
-                w[u] = j < v_hi ? load_vector(vectors + j) : make_uint4(none, none, none, none);
+                constexpr uint32_t kNone = DTYPE == SBW_DTYPE_F32 ? 0xff800000u : 0xff80ff80u;
+                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(slots + slot + u * (kThreads * 16))
+                                                                : make_uint4(kNone, kNone, kNone, kNone);
             }
-            float vm[U];
-            float mx = -INFINITY;
+            slot = next_slot(slot);
+            if constexpr (INSIDE) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t col = layout.head + (j0 + u * kThreads) * VEC;
-                bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col, a.bias);
-                vm[u] = vector_max<DTYPE>(w[u]);
-                mx = fmaxf(mx, vm[u]);
+                for (int u = 0; u < U; ++u) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+                copy_commit();
+                src += U * kThreads;
+                src_slot = next_slot(src_slot);
+            } else {
+                copy_checked();
             }
-            if (mx > st.m) st.move(mx, c);
-            const uint64_t nm2 = pack2(-st.m, -st.m);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int i = 0; i < VEC; i += 2) {
-                    float x0, x1;
-                    unpack2(mul2(add2(pack2(element<DTYPE>(w[u], i), element<DTYPE>(w[u], i + 1)), nm2), c2), x0, x1);
-                    x0 = max_nan(x0, kFar);
-                    x1 = max_nan(x1, kFar);
-                    const uint64_t e = pack2(ex2_approx_ftz(x0), ex2_approx_ftz(x1));
-                    z2 = add2(z2, e);
-                    s2 = fma2(e, pack2(x0, x1), s2);
-                }
-                if (vm[u] >= bar) {
-                    const uint32_t col = layout.head + (j0 + u * kThreads) * VEC;
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        const float x = element<DTYPE>(w[u], i);
-                        if (x > bar || (x == bar && col + i < t)) st.above += 1u;
-                    }
-                }
-            }
-            fold();                                      // short chains of additions: a trip's, then the trips'
+            const uint32_t col0 = share.head + j0 * VEC;
+            bias_vectors<DTYPE, SCHEME, U>(w, rs, a.vocab_offset + col0, kThreads * VEC, a.bias);
+            const float mx = largest_of<DTYPE, U>(w);
+            if (mx > st.top) raise(mx);
             if constexpr (TOP) {
-                if (trip == 0) {
-                    // the top_n-th largest of 128 maxima of disjoint column sets bounds this part's
-                    // alternatives from below; known after the first trip
-                    float g = fmaxf(mx, xe);
-                    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
-                    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-                    if ((lane & 3) == 0) sh_group[tid >> 2] = g;
-                    if (tid == 0) sh_count = 0;
-                    __syncthreads();
-                    if (tid < static_cast<unsigned>(kGroups)) {
-                        const float mine = sh_group[tid];
-                        int rank = 0;
-                        for (int o = 0; o < kGroups; ++o) {
-                            const float other = sh_group[o];
-                            rank += (other > mine || (other == mine && o < static_cast<int>(tid))) ? 1 : 0;
-                        }
-                        if (rank == a.top_n - 1) sh_floor = mine;
+                if (trip == 0 || trip == 4) new_floor(st.top);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t *e = reinterpret_cast<const uint32_t *>(&w[u]);
+                if constexpr (DTYPE == SBW_DTYPE_F32) {
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2)
+                        add_pair(max_nan(__uint_as_float(e[i]), least), max_nan(__uint_as_float(e[i + 1]), least));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t q = max_nan_bf16x2(e[i], least2);
+                        add_pair(__uint_as_float(q << 16), __uint_as_float(q & 0xffff0000u));
                     }
-                    __syncthreads();
-                    floor = sh_floor;
-                    if (ce < V) push(xe, ce);
                 }
+            }
+            if (mx >= bar) {                                     // some column may rank before the token
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (vm[u] >= floor && j0 + u * kThreads < v_hi) {
-                        const uint32_t col = layout.head + (j0 + u * kThreads) * VEC;
+                    const uint32_t col = col0 + u * (kThreads * VEC);
+                    if (t - col < static_cast<uint32_t>(VEC)) {  // the token's own vector
 #pragma unroll
-                        for (int i = 0; i < VEC; ++i) push(element<DTYPE>(w[u], i), col + i);
+                        for (int i = 0; i < VEC; ++i) {
+                            const float x = element<DTYPE>(w[u], i);
+                            if (x > bar || (x == bar && col + i < t)) count += 1.0f;
+                        }
+                    } else if constexpr (DTYPE == SBW_DTYPE_F32) {
+                        const float limit = col < t ? below : bar;
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i)
+                            if (element<DTYPE>(w[u], i) > limit) count += 1.0f;
+                    } else {
+                        const uint32_t limit = col < t ? below2 : bar2;
+                        const __nv_bfloat162 l2 = *reinterpret_cast<const __nv_bfloat162 *>(&limit);
+                        const __nv_bfloat162 *q = reinterpret_cast<const __nv_bfloat162 *>(&w[u]);
+                        const __nv_bfloat162 n = __hadd2(__hadd2(__hgt2(q[0], l2), __hgt2(q[1], l2)),
+                                                         __hadd2(__hgt2(q[2], l2), __hgt2(q[3], l2)));
+                        count += __low2float(n) + __high2float(n);
                     }
                 }
             }
+            if constexpr (TOP) {
+                if (mx >= floor) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (vector_max<DTYPE>(w[u]) >= floor && j0 + u * kThreads < share.v_hi) {
+                            const uint32_t col = col0 + u * (kThreads * VEC);
+#pragma unroll
+                            for (int i = 0; i < VEC; ++i) push(element<DTYPE>(w[u], i), col + i);
+                        }
+                    }
+                }
+            }
+            fold();                                              // short chains of additions: a trip's, then the trips'
+            ++trip;
+            j0 += U * kThreads;
+        };
+        const uint32_t trips = share.template trips<U * kThreads>();
+        const uint32_t full = (share.v_hi - share.v_lo) / (U * kThreads);
+        constexpr uint32_t kAhead = R::kStages - 1;
+        if (full > kAhead) {
+            const uint32_t inside = full - kAhead;               // the copies are kAhead groups ahead, in this row
+            while (trip < inside) trip_body(std::true_type{});
+            src_left -= static_cast<int>(inside * (U * kThreads));
+            src_groups -= inside;
         }
+        while (trip < trips) trip_body(std::false_type{});
+        const int64_t row_ahead = next_real(row + step, token_ahead);
+
+        if (ce < V) {
+            if (xe > st.top) raise(xe);
+            add_pair(max_nan(xe, least), 0.0f);
+            z2.y = s2.y = 0.0f;
+            fold();
+            if (xe > bar || (xe == bar && ce < t)) count += 1.0f;
+            if constexpr (TOP) push(xe, ce);
+        }
+        st.above = static_cast<uint32_t>(count);
         if (t_nothing) st.above = count_above_nothing<DTYPE, SCHEME>(a, row, c_lo, c_hi, t);
 
-        // ---- this part's sums ----
+        [[maybe_unused]] const float largest = st.top;           // of the thread's columns
+        // ---- this warp's sums, to CTA 0 ----
         {
-            float m = st.m;
-            for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            st.move(m, c);
+            for (int d = 16; d > 0; d >>= 1) st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
+            st.move(fmaxf(st.top, kNoValue) * c);
             for (int d = 16; d > 0; d >>= 1) {
                 st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
                 st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
-                st.above += __shfl_xor_sync(0xffffffffu, st.above, d);
             }
-            if (lane == 0) sh_warp[warp] = st;
-        }
-        __syncthreads();
-        if (tid == 0) {
-            float m = sh_warp[0].m;
-            for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sh_warp[w].m);
-            Stats sum = {m, 0.0f, 0.0f, 0u};
-            for (int w = 0; w < kWarps; ++w) {
-                Stats p = sh_warp[w];
-                p.move(m, c);
-                sum.z += p.z;
-                sum.s += p.s;
-                sum.above += p.above;
-            }
-            sh_part = sum;
+            st.above = __reduce_add_sync(0xffffffffu, st.above);
+            if (parts > 1) cluster.barrier_wait();               // CTA 0 runs
+            if (lane == 0) *cluster.map_shared_rank(&sh_warp[buf][part * kWarps + warp], 0) = st;
         }
 
         // ---- this part's alternatives ----
         if constexpr (TOP) {
-            unsigned n = sh_count;
             const unsigned need = min(static_cast<unsigned>(a.top_n), c_hi - c_lo);
-            bool strict = !(floor > -INFINITY);          // the list holds what is above the floor, not what equals it
-            if (n > static_cast<unsigned>(kCap) && !strict) {
-                __syncthreads();                         // everyone has read the count
+            new_floor(largest);                                  // every push is in the list now
+            unsigned n = sh_count;
+            bool strict = !(floor > -INFINITY);                  // the list holds what is above the floor, not what equals it
+            for (int again = 0; again < 2 && n > static_cast<unsigned>(kCap) && !(again == 1 && strict); ++again) {
+                __syncthreads();                                 // everyone has read the count
                 if (tid == 0) sh_count = 0;
                 __syncthreads();
-                gather_above<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, sh_list, &sh_count);
+                strict = strict || again == 1;
+                gather_again<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, strict, sh_list, &sh_count);
                 __syncthreads();
                 n = sh_count;
-                strict = true;
             }
-            for (unsigned i = tid; i < static_cast<unsigned>(kMaxTop); i += kThreads) sh_top[i] = 0;
-            __syncthreads();
+            for (unsigned i = tid; i < need; i += kThreads) sh_top[i] = 0;
             if (n <= static_cast<unsigned>(kCap)) {
+                const uint64_t least = static_cast<uint64_t>(value_code(floor)) << 32;
                 for (unsigned i = tid; i < n; i += kThreads) {
                     const uint64_t mine = sh_list[i];
-                    unsigned rank = 0;
-#pragma unroll 4
-                    for (unsigned o = 0; o < n; ++o) rank += sh_list[o] > mine ? 1u : 0u;
+                    if (mine >= least) {
+                        const unsigned pos = atomicAdd(&sh_kept, 1u);
+                        if (pos < static_cast<unsigned>(kKeep)) sh_keep[pos] = mine;
+                    }
+                }
+                __syncthreads();
+                const unsigned kept = sh_kept;
+                const bool few = kept <= static_cast<unsigned>(kKeep);
+                const uint64_t *list = few ? sh_keep : sh_list;
+                const unsigned count = few ? kept : n;
+                for (unsigned i = tid; i < count; i += kThreads) {
+                    const uint64_t mine = list[i];
+                    const unsigned rank = count_larger(list, count, mine);
                     if (rank < need) sh_top[rank] = mine;
                 }
-                if (n < need && warp == 0) fill_equal<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, sh_top, n, need);
+                if (count < need && warp == 0) fill_equal<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, sh_top, count, need);
             } else {
-                select_rounds<DTYPE, SCHEME>(a, row, c_lo, c_hi, sh_top, need, sh_scratch);
+                __syncthreads();
+                select_rounds<DTYPE, SCHEME>(a, row, c_lo, c_hi, sh_top, need, sh_keep);
             }
+            __syncthreads();
+            if (tid == 0) sh_count = sh_kept = sh_floor = 0;     // for the next row, whose first barrier comes before any use
+            if (parts > 1)
+                for (unsigned i = tid; i < static_cast<unsigned>(a.top_n); i += kThreads)
+                    *cluster.map_shared_rank(&sh_all[part * a.top_n + i], 0) = i < need ? sh_top[i] : 0;
         }
-        __syncthreads();
+        if (parts > 1) cluster.sync();                           // everything has arrived in CTA 0
+        else if (!TOP) __syncthreads();
 
         // ---- the row ----
-        cluster.sync();
+        const Stats *sums = sh_warp[buf];
+        const unsigned n_sums = parts * kWarps;
+        float m = -INFINITY;                                     // the row's largest value
         if (part == 0) {
+            for (unsigned i = lane; i < n_sums; i += 32) m = fmaxf(m, sums[i].top);
+            for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        }
+        const bool nothing = m == -INFINITY, ordinary = fabsf(m) < kOrdinary;
+        Stats plain = {};
+        if (part == 0 && !nothing && !ordinary) plain = sum_plainly<DTYPE, SCHEME>(a, row, 0u, V, m, sh_scratch);
+        if (part == 0 && (parts > 1 || warp == 0)) {             // every warp the same
             double z = 0.0, s = 0.0;
             uint32_t above = 0;
-            float m = sh_part.m;
-            for (unsigned r = 1; r < parts; ++r) m = fmaxf(m, cluster.map_shared_rank(&sh_part, r)->m);
-            for (unsigned r = 0; r < parts; ++r) {
-                Stats p = *cluster.map_shared_rank(&sh_part, r);
-                p.move(m, c);
+            const float ref = ordinary ? m * c : 0.0f;
+            for (unsigned i = lane; i < n_sums; i += 32) {
+                Stats p = sums[i];
+                above += p.above;
+                p.move(ref);
                 z += static_cast<double>(p.z);
                 s += static_cast<double>(p.s);
-                above += p.above;
             }
-            const bool nothing = z == 0.0;               // every logit is -inf
+            for (int d = 16; d > 0; d >>= 1) {
+                z += __shfl_xor_sync(0xffffffffu, z, d);
+                s += __shfl_xor_sync(0xffffffffu, s, d);
+            }
+            above = __reduce_add_sync(0xffffffffu, above);
+            if (nothing) {
+                z = z == z ? 0.0 : z;                            // NaN and -inf alone: NaN
+            } else if (ordinary) {
+                // relative to m itself from here on: the terms are 2^((l - m) c) 2^(m c - ref)
+                const double d = static_cast<double>(m) * static_cast<double>(c) - static_cast<double>(ref);
+                s -= d * z;
+                const double f = exp2(-d);
+                z *= f;
+                s *= f;
+            } else {
+                z = plain.z;
+                s = plain.s;
+            }
             const double ln_z = log(z);
-            const double inv_tau = 1.0 / a.tau;
             auto logp = [&](float x) -> float {
-                if (nothing) return -INFINITY;
-                return static_cast<float>((static_cast<double>(x) - static_cast<double>(m)) * inv_tau - ln_z);
+                if (z == 0.0) return -INFINITY;                  // every logit is -inf
+                return static_cast<float>((static_cast<double>(x) - static_cast<double>(m)) * a.inv_tau - ln_z);
             };
             if (tid == 0) {
                 if (a.out_logprob) a.out_logprob[row] = logp(xt);
                 if (a.out_entropy)
-                    a.out_entropy[row] = nothing ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
+                    a.out_entropy[row] = z == 0.0 ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
                 if (a.out_rank) a.out_rank[row] = 1 + static_cast<int32_t>(above);
-                const bool bad = z != z;                 // a NaN or +inf among the logits
-                if (a.out_max) a.out_max[row] = bad ? NAN : nothing ? -INFINITY : m;
+                const bool bad = z != z;                         // a NaN or +inf among the logits
+                if (a.out_max) a.out_max[row] = bad ? NAN : m;
                 if (a.out_sumexp) a.out_sumexp[row] = static_cast<float>(z);
             }
             if constexpr (TOP) {
-                const unsigned n = a.top_n, all = n * parts;
-                for (unsigned i = tid; i < all; i += kThreads) sh_all[i] = cluster.map_shared_rank(&sh_top[0], i / n)[i % n];
-                for (unsigned i = tid; i < n; i += kThreads) {       // places no column takes
-                    if (i >= V) {
-                        if (a.out_top_ids) a.out_top_ids[row * n + i] = -1;
-                        if (a.out_top_logprobs) a.out_top_logprobs[row * n + i] = -INFINITY;
-                    }
-                }
-                __syncthreads();
-                for (unsigned i = tid; i < all; i += kThreads) {
-                    const uint64_t mine = sh_all[i];
+                const unsigned n = a.top_n, all = parts > 1 ? n * parts : min(n, V);
+                const uint64_t *list = parts > 1 ? sh_all : sh_top;
+                for (unsigned i = tid; i < all; i += parts > 1 ? kThreads : 32) {
+                    const uint64_t mine = list[i];
                     if (mine == 0) continue;
-                    unsigned rank = 0;
-                    if (parts == 1) rank = i;
-                    else
-                        for (unsigned o = 0; o < all; ++o) rank += sh_all[o] > mine ? 1u : 0u;
+                    unsigned rank = i;
+                    if (parts > 1) rank = count_larger(list, all, mine);
                     if (rank < n) {
                         if (a.out_top_ids) a.out_top_ids[row * n + rank] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(mine));
                         if (a.out_top_logprobs) a.out_top_logprobs[row * n + rank] = logp(composite_value(mine));
                     }
                 }
+                for (unsigned i = V + tid; i < n; i += parts > 1 ? kThreads : 32) {   // places no column takes
+                    if (a.out_top_ids) a.out_top_ids[row * n + i] = -1;
+                    if (a.out_top_logprobs) a.out_top_logprobs[row * n + i] = -INFINITY;
+                }
             }
         }
-        cluster.sync();                                  // the other parts' shared memory has been read
+        buf ^= 1;
+        row = row_ahead;
     }
+    copy_wait<0>();
 }
 
 // Gradient: no reduction, so a row is cut into blocks of kGradVectors vectors per thread and every
@@ -608,7 +853,7 @@ logprob_backward_kernel(const GradArgs a) {
 #pragma unroll
         for (int u = 0; u < kGradVectors; ++u) {
             const uint32_t j = first + u * kGradThreads;
-            if (j < layout.nvec) w[u] = load_vector_rw(vectors + j);
+            if (j < layout.nvec) w[u] = load_vector(vectors + j);
         }
     }
 #pragma unroll
@@ -675,7 +920,7 @@ int check_common(const Common &q, bool *marked) {
     if (!(q.temperature > 0.0f) || q.temperature - q.temperature != 0.0f) return SBW_ERR_INVALID_ARG;
     if (!(q.delta == q.delta) || q.delta - q.delta != 0.0f) return SBW_ERR_INVALID_ARG;
     const double c = 1.4426950408889634 / static_cast<double>(q.temperature);
-    if (!(c > 1e-30 && c < 1e23)) return SBW_ERR_INVALID_ARG;      // temperature too small or too large for fp32 exponents
+    if (!(c > 1.4e-6 && c < 1.5e6)) return SBW_ERR_INVALID_ARG;    // temperature outside 1e-6 .. 1e6
     if (q.V > 0x7fffffffLL || q.vocab_offset + q.V > (int64_t(1) << 32)) return SBW_ERR_UNSUPPORTED;
     const float in_precision = q.dtype == SBW_DTYPE_BF16 ? __bfloat162float(__float2bfloat16_rn(q.delta)) : q.delta;
     *marked = in_precision != 0.0f;
@@ -700,17 +945,47 @@ BiasParams bias_params(const Common &q) {
     return p;
 }
 
+// CTAs per row.  Without the hash the rows' bytes bound the call: as many CTAs as are resident at once,
+// no more (a row's CTAs should find at least one trip each).  With it the SMs' multipliers do: the
+// fewest CTAs per row whose total comes within 3 % of the best share-out over the SMs.
+int parts_per_row(int64_t B, int64_t nvec, int64_t per_trip, int sm_count, int scheme, int most_parts) {
+    int64_t most = (nvec + per_trip - 1) / per_trip;
+    if (most > most_parts) most = most_parts;
+    if (most < 1) most = 1;
+    if (scheme < 0) {
+        const int64_t fill = static_cast<int64_t>(sm_count) * ctas_per_sm(scheme) / B;
+        return static_cast<int>(fill < 1 ? 1 : fill < most ? fill : most);
+    }
+    int best = 1;
+    double best_eff = 0.0;
+    for (int64_t p = 1; p <= most; ++p) {
+        const int64_t ctas = B * p, waves = (ctas + sm_count - 1) / sm_count;
+        const double eff = static_cast<double>(ctas) / static_cast<double>(waves * sm_count);
+        if (eff > best_eff + 0.03) { best_eff = eff; best = static_cast<int>(p); }
+    }
+    return best;
+}
+
 template <int DTYPE, int SCHEME, bool TOP>
 int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     DeviceInfo di;
     if (int rc = current_device_info(&di)) return rc;
-    const int64_t resident = static_cast<int64_t>(di.sm_count) * (SCHEME == kSchemeNone ? 2 : 1);
-    int parts = 1;
-    while (parts < kMaxCluster && a.B * parts * 2 <= resident && a.V >= 4096 * parts) parts *= 2;
+    using R = Ring<SCHEME, TOP>;
+    const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP>;
+    // clusters above 8 CTAs and that much shared memory have to be asked for, once per device
+    static std::atomic<uint64_t> prepared{0};
+    if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
+    if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
+        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kBytes));
+        prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
+    }
+    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(SCHEME, TOP));
+    const int64_t resident = static_cast<int64_t>(di.sm_count) * ctas_per_sm(SCHEME);
     cudaLaunchConfig_t cfg = {};
-    const int64_t ctas = parts > 1 ? a.B * parts : (a.B < resident ? a.B : resident);
-    cfg.gridDim = dim3(static_cast<unsigned>(ctas));
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3(static_cast<unsigned>(parts > 1 ? a.B * parts : (a.B < resident ? a.B : resident)));
+    cfg.blockDim = dim3(R::kThreads);
+    cfg.dynamicSmemBytes = R::kBytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -719,7 +994,7 @@ int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, logprob_kernel<DTYPE, SCHEME, TOP>, a));
+    SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return SBW_OK;
 }
 
@@ -787,7 +1062,7 @@ extern "C" int sbw_token_logprobs(const void *logits, int dtype, int64_t B, int6
     a.W = ctx_width;
     a.vocab_offset = static_cast<uint32_t>(vocab_offset);
     a.bias = bias_params(q);
-    a.tau = static_cast<double>(temperature);
+    a.inv_tau = 1.0 / static_cast<double>(temperature);
     a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
     a.tokens = tokens;
     a.top_n = static_cast<int>(top_n);
