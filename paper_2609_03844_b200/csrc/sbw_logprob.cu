@@ -30,10 +30,11 @@ namespace {
 __host__ __device__ constexpr int threads_of(int scheme) { return scheme < 0 ? 256 : 128; }
 __host__ __device__ constexpr int ctas_per_sm(int scheme) { return scheme < 0 ? 3 : 4; }
 constexpr int kCap = 1280;              // candidate list entries
-constexpr int kKeep = 256;              // candidates left after the last cut, for the fast ranking
+constexpr int kBlocks = 8;              // blocks of steps whose maxima a thread remembers
+constexpr int kHits = 512;              // blocks that reach the bound
 constexpr int kMaxTop = SBW_MAX_TOP_LOGPROBS;
 // CTAs per row at most
-__host__ __device__ constexpr int max_parts(int scheme, bool top) { return scheme < 0 && top ? 8 : 16; }
+__host__ __device__ constexpr int max_parts(int scheme, bool top) { return top ? 8 : 16; }
 constexpr float kFar = -300.0f;         // exponents below this give 2^x = 0; keeps 0 * inf out of the sums
 static_assert(kCap >= 16 * kMaxTop + 16, "a share with vectors for fewer groups than alternatives must fit the list");
 
@@ -278,10 +279,12 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
 // Every thread copies its own vectors into its own slots of shared memory, groups of a few vectors
 // some groups ahead (cp.async: no register waits for the data, no barrier, and a thread waits for
 // nothing but its own copies), across row boundaries too, so that the loads go on while a row is finished.
-template <int SCHEME, bool TOP>
+template <int DTYPE, int SCHEME, bool TOP>
 struct Ring {
-    static constexpr int kGroup = SCHEME == kSchemeNone ? 4 : 2;             // vectors of a group; a trip takes one group
-    static constexpr int kStages = SCHEME == kSchemeNone && TOP ? 2 : 3;
+    static constexpr int kStep = SCHEME == kSchemeNone ? 4 : 2;              // vectors taken at a time
+    static constexpr int kSteps = SCHEME == kSchemeNone ? 1 : TOP ? 2 : 4;   // steps of a trip; a trip takes one group of copies
+    static constexpr int kGroup = kStep * kSteps;
+    static constexpr int kStages = SCHEME == kSchemeNone ? 3 : 2;
     static constexpr int kThreads = threads_of(SCHEME);
     static constexpr int kGroupBytes = kGroup * kThreads * 16;
     static constexpr int kBytes = kGroupBytes * kStages;
@@ -311,8 +314,9 @@ struct Share {
         const RowLayout<DTYPE> layout(row_ptr, static_cast<uint32_t>(a.V));
         head = layout.head;
         vectors = reinterpret_cast<const uint4 *>(row_ptr + static_cast<size_t>(head) * RowLayout<DTYPE>::ESIZE);
-        v_lo = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * part / parts);
-        v_hi = static_cast<uint32_t>(static_cast<uint64_t>(layout.nvec) * (part + 1) / parts);
+        const uint32_t q = layout.nvec / parts, extra = layout.nvec - q * parts;
+        v_lo = q * part + min(part, extra);
+        v_hi = v_lo + q + (part < extra ? 1u : 0u);
     }
     template <uint32_t PER_TRIP>
     __device__ __forceinline__ uint32_t trips() const {
@@ -320,21 +324,24 @@ struct Share {
     }
 };
 
-// The largest value that at least n of the group maxima reach, by the first `groups` threads; needs
-// barriers on both sides.
-__device__ __forceinline__ void bound_below(const float *group, int groups, int n, unsigned *out) {
-    const int i = threadIdx.x;
-    if (i >= groups) return;
-    const float mine = group[i];
-    int reach = 0;
-    const float4 *g4 = reinterpret_cast<const float4 *>(group);
-#pragma unroll 8
-    for (int o = 0; o < groups / 4; ++o) {
+// The largest of the group maxima that at least n of them reach (code of -inf or less if there is none), of
+// this warp's groups.  The threads of a group -- `members` neighbours, which all hand over its maximum --
+// share the comparisons out.
+__device__ __forceinline__ unsigned bound_below(const float *group, int groups, unsigned members, float mine, int n) {
+    const int share = groups / static_cast<int>(members);        // a multiple of 4
+    const float4 *g4 = reinterpret_cast<const float4 *>(group + (threadIdx.x & (members - 1)) * share);
+    int r0 = 0, r1 = 0, r2 = 0, r3 = 0;
+#pragma unroll 4
+    for (int o = 0; o < share / 4; ++o) {
         const float4 g = g4[o];
-        reach += (g.x >= mine ? 1 : 0) + (g.y >= mine ? 1 : 0) + (g.z >= mine ? 1 : 0) + (g.w >= mine ? 1 : 0);
+        r0 += g.x >= mine ? 1 : 0;
+        r1 += g.y >= mine ? 1 : 0;
+        r2 += g.z >= mine ? 1 : 0;
+        r3 += g.w >= mine ? 1 : 0;
     }
-    const unsigned best = __reduce_max_sync(0xffffffffu, reach >= n ? value_code(mine) : 0u);
-    if ((i & 31) == 0) atomicMax(out, best);
+    int reach = r0 + r1 + r2 + r3;
+    for (unsigned d = 1; d < members; d <<= 1) reach += __shfl_xor_sync(0xffffffffu, reach, d);
+    return __reduce_max_sync(0xffffffffu, reach >= n ? value_code(mine) : 0u);
 }
 
 // Entries of a 16-byte aligned list that are larger than `mine`.
@@ -361,15 +368,18 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     namespace cg = cooperative_groups;
     using Layout = RowLayout<DTYPE>;
     constexpr int VEC = Layout::VEC;
-    using R = Ring<SCHEME, TOP>;
-    constexpr int U = R::kGroup, kThreads = R::kThreads, kWarps = kThreads / 32;
+    using R = Ring<DTYPE, SCHEME, TOP>;
+    constexpr int U = R::kStep, kPerTrip = R::kGroup * R::kThreads, kThreads = R::kThreads, kWarps = kThreads / 32;
     extern __shared__ __align__(16) unsigned char sh_ring[];
     __shared__ Stats sh_warp[2][max_parts(SCHEME, TOP) * kWarps];            // of two rows in turn
     __shared__ Stats sh_scratch[kWarps];
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
-    __shared__ unsigned sh_floor, sh_count, sh_kept;
+    __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
+    __shared__ double sh_row[3];                                 // of the row being finished: largest value, ln Z, Z
+    __shared__ uint16_t sh_hit[TOP ? kHits : 1];
+    __shared__ float sh_block[TOP ? kBlocks : 1][kThreads];
     __shared__ __align__(16) uint64_t sh_list[TOP ? kCap : 1];
-    __shared__ __align__(16) uint64_t sh_keep[TOP ? kKeep : kWarps];
+    __shared__ uint64_t sh_rounds[kWarps];
     __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];               // this part's alternatives, best first, 0 = none
     __shared__ __align__(16) uint64_t sh_all[TOP ? kMaxTop * max_parts(SCHEME, TOP) : 1];  // every part's, in CTA 0
 
@@ -379,10 +389,10 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     const float c = a.c;
     const unsigned tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t step = gridDim.x / parts;
-    const int groups = a.top_n <= 32 ? 64 : 128;                 // sets of columns whose maxima bound the alternatives
+    const int groups = a.top_n <= 8 ? 32 : a.top_n <= 32 ? 64 : 128;                // sets of columns whose maxima bound the alternatives
     if (parts > 1) cluster.barrier_arrive();                     // waited for before another CTA's memory is written
 
-    if (TOP && tid == 0) sh_count = sh_kept = sh_floor = 0;
+    if (TOP && tid == 0) sh_count = sh_hits = 0;
     const float far = 300.0f / c;
     int buf = 0;
 
@@ -412,7 +422,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     // The copying side: the next group's first vector of this thread, how many vectors the share has from
     // there on, and how many groups.
     const uint32_t slots = static_cast<uint32_t>(__cvta_generic_to_shared(sh_ring)) + tid * 16;
-    int64_t src_row = static_cast<int64_t>(blockIdx.x / parts) - step;
+    const int64_t first_row = blockIdx.x / parts;
+    int64_t src_row = first_row - step;
     const uint4 *src = nullptr;
     int src_left = 0;
     uint32_t src_groups = 0, src_slot = 0;
@@ -420,22 +431,22 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     auto copy_checked = [&]() {
         if (src_groups == 0) {                                   // on to the next row that is not padded
             do src_row += step;
-            while (parts == 1 && src_row < a.B && a.tokens && static_cast<uint32_t>(a.tokens[src_row]) >= V);
+            while (src_row != first_row && src_row < a.B && a.tokens && static_cast<uint32_t>(a.tokens[src_row]) >= V);
             src_left = 0;
             src_groups = 0xffffffffu;                            // after the last row: empty groups
             if (src_row < a.B) {
                 const Share<DTYPE> share(a, src_row, part, parts);
                 src = share.vectors + share.v_lo + tid;
                 src_left = static_cast<int>(share.v_hi - share.v_lo - tid);
-                src_groups = share.template trips<U * kThreads>();
+                src_groups = share.template trips<kPerTrip>();
             }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < R::kGroup; ++u)
             if (src_left > u * kThreads) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
         copy_commit();
-        src += U * kThreads;
-        src_left -= U * kThreads;
+        src += kPerTrip;
+        src_left -= kPerTrip;
         --src_groups;
         src_slot = next_slot(src_slot);
     };
@@ -443,8 +454,15 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     for (int i = 0; i < R::kStages - 1; ++i) copy_checked();
     uint32_t slot = 0;
 
-    int64_t row = blockIdx.x / parts;
+    int64_t row = first_row;                                     // copied before its token was known
     uint32_t t = token_of(row);
+    if (parts == 1 && a.tokens && t >= V) {                      // padded: begin again after it
+        copy_wait<0>();
+        src_row = first_row;
+        src_groups = src_slot = 0;
+#pragma unroll 1
+        for (int i = 0; i < R::kStages - 1; ++i) copy_checked();
+    }
     row = next_real(row, t);
     if (row >= a.B && parts > 1) cluster.barrier_wait();
 
@@ -480,25 +498,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         float least = kNoValue;                                  // values below count as this
         [[maybe_unused]] uint32_t least2 = both_halves(kNoValue);
         float count = 0.0f;                                      // columns that rank before the token
-        float floor = INFINITY;                                  // alternatives have at least this value
-
-        auto push = [&](float x, uint32_t col) {
-            if (x >= floor && x > -INFINITY) {
-                const unsigned pos = atomicAdd(&sh_count, 1u);
-                if (pos < static_cast<unsigned>(kCap)) sh_list[pos] = composite(x, col);
-            }
-        };
-        auto new_floor = [&](float with) {                       // two barriers
-            const int members = kThreads / groups;               // 4, 2 or 1 threads
-            float g = with;
-            if (members > 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
-            if (members > 2) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-            if ((tid & (members - 1)) == 0) sh_group[tid / members] = g;
-            __syncthreads();
-            bound_below(sh_group, groups, a.top_n, &sh_floor);
-            __syncthreads();
-            floor = __uint_as_float(order_decode(sh_floor));     // at least n columns reach it; -inf: perhaps not
-        };
+        [[maybe_unused]] float block_top = -INFINITY;            // largest value of the block of steps
         float2 z2 = {0.0f, 0.0f}, s2 = {0.0f, 0.0f};             // partial sums of the trip
         auto fold = [&]() {
             st.z += z2.x + z2.y;
@@ -514,41 +514,47 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
             }
         };
-        // two columns in each operation
+        // Two columns at a time: in packed operations, or, with the hash, in plain ones, which leave the half
+        // of the FMA pipe that multiplies integers to the hash.
         auto add_pair = [&](float l0, float l1) {
+            if constexpr (SCHEME != kSchemeNone) {
+                const float x0 = fmaf(l0, c, -st.ref), x1 = fmaf(l1, c, -st.ref);
+                const float e0 = ex2_approx_ftz(x0), e1 = ex2_approx_ftz(x1);
+                z2 = make_float2(z2.x + e0, z2.y + e1);
+                s2 = make_float2(fmaf(e0, x0, s2.x), fmaf(e1, x1, s2.y));
+                return;
+            }
             const float2 x = __ffma2_rn(make_float2(l0, l1), make_float2(c, c), make_float2(-st.ref, -st.ref));
             const float2 e = make_float2(ex2_approx_ftz(x.x), ex2_approx_ftz(x.y));
             z2 = __fadd2_rn(z2, e);
             s2 = __ffma2_rn(e, x, s2);
         };
-        uint32_t trip = 0;
-        uint32_t j0 = share.v_lo + tid;                          // this trip's first vector
-        auto trip_body = [&](const auto inside_tag) {
-            constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
+        uint32_t trip = 0, step_no = 0;
+        uint32_t j0 = share.v_lo + tid;                          // this step's first vector
+        const uint32_t trips = share.template trips<kPerTrip>();
+        int block_shift = 0;                                     // steps of a block: 2^block_shift
+        if constexpr (TOP) {
+            while (trips * R::kSteps > static_cast<uint32_t>(kBlocks) << block_shift) ++block_shift;
+        }
+        auto step_body = [&](const uint32_t from, const auto inside_tag) {
+            constexpr bool INSIDE = decltype(inside_tag)::value;
             uint4 w[U];
-            copy_wait<R::kStages - 2>();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 constexpr uint32_t kNone = DTYPE == SBW_DTYPE_F32 ? 0xff800000u : 0xff80ff80u;
-                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(slots + slot + u * (kThreads * 16))
+                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(from + u * (kThreads * 16))
                                                                 : make_uint4(kNone, kNone, kNone, kNone);
-            }
-            slot = next_slot(slot);
-            if constexpr (INSIDE) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
-                copy_commit();
-                src += U * kThreads;
-                src_slot = next_slot(src_slot);
-            } else {
-                copy_checked();
             }
             const uint32_t col0 = share.head + j0 * VEC;
             bias_vectors<DTYPE, SCHEME, U>(w, rs, a.vocab_offset + col0, kThreads * VEC, a.bias);
             const float mx = largest_of<DTYPE, U>(w);
             if (mx > st.top) raise(mx);
             if constexpr (TOP) {
-                if (trip == 0 || trip == 4) new_floor(st.top);
+                block_top = fmaxf(block_top, mx);
+                if ((step_no + 1) >> block_shift != step_no >> block_shift) {
+                    sh_block[step_no >> block_shift][tid] = block_top;
+                    block_top = -INFINITY;
+                }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -590,29 +596,37 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                     }
                 }
             }
-            if constexpr (TOP) {
-                if (mx >= floor) {
+        };
+        auto trip_body = [&](const auto inside_tag) {
+            constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
+            copy_wait<R::kStages - 2>();
+            const uint32_t here = slots + slot;
+            slot = next_slot(slot);
+            if constexpr (INSIDE) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (vector_max<DTYPE>(w[u]) >= floor && j0 + u * kThreads < share.v_hi) {
-                            const uint32_t col = col0 + u * (kThreads * VEC);
-#pragma unroll
-                            for (int i = 0; i < VEC; ++i) push(element<DTYPE>(w[u], i), col + i);
-                        }
-                    }
-                }
+                for (int u = 0; u < R::kGroup; ++u) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+                copy_commit();
+                src += kPerTrip;
+                src_slot = next_slot(src_slot);
+            } else {
+                copy_checked();
+            }
+#pragma unroll 1
+            for (int k = 0; k < R::kSteps; ++k) {
+                if (!INSIDE && j0 - tid >= share.v_hi && k > 0) break;   // the share ends before this step
+                step_body(here + k * (U * kThreads * 16), inside_tag);
+                ++step_no;
+                j0 += U * kThreads;
             }
             fold();                                              // short chains of additions: a trip's, then the trips'
             ++trip;
-            j0 += U * kThreads;
         };
-        const uint32_t trips = share.template trips<U * kThreads>();
-        const uint32_t full = (share.v_hi - share.v_lo) / (U * kThreads);
+        const uint32_t full = (share.v_hi - share.v_lo) / kPerTrip;
         constexpr uint32_t kAhead = R::kStages - 1;
         if (full > kAhead) {
             const uint32_t inside = full - kAhead;               // the copies are kAhead groups ahead, in this row
             while (trip < inside) trip_body(std::true_type{});
-            src_left -= static_cast<int>(inside * (U * kThreads));
+            src_left -= static_cast<int>(inside * kPerTrip);
             src_groups -= inside;
         }
         while (trip < trips) trip_body(std::false_type{});
@@ -624,12 +638,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             z2.y = s2.y = 0.0f;
             fold();
             if (xe > bar || (xe == bar && ce < t)) count += 1.0f;
-            if constexpr (TOP) push(xe, ce);
         }
         st.above = static_cast<uint32_t>(count);
         if (t_nothing) st.above = count_above_nothing<DTYPE, SCHEME>(a, row, c_lo, c_hi, t);
 
         [[maybe_unused]] const float largest = st.top;           // of the thread's columns
+        if (TOP && (step_no >> block_shift) < kBlocks) sh_block[step_no >> block_shift][tid] = block_top;
         // ---- this warp's sums, to CTA 0 ----
         {
             for (int d = 16; d > 0; d >>= 1) st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
@@ -646,7 +660,51 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         // ---- this part's alternatives ----
         if constexpr (TOP) {
             const unsigned need = min(static_cast<unsigned>(a.top_n), c_hi - c_lo);
-            new_floor(largest);                                  // every push is in the list now
+            // a value that top_n columns of this part reach, from the maxima of disjoint sets of them
+            const unsigned members = kThreads / groups;          // 8, 4, 2 or 1 threads
+            float g = largest;
+            for (unsigned d = 1; d < members; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+            if ((tid & (members - 1)) == 0) sh_group[tid / members] = g;
+            __syncthreads();
+            const unsigned best = bound_below(sh_group, groups, members, g, a.top_n);
+            if (lane == 0) sh_floor[warp] = best;
+            __syncthreads();
+            unsigned floor_code = sh_floor[0];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) floor_code = max(floor_code, sh_floor[w]);
+            const float floor = __uint_as_float(order_decode(floor_code));   // -inf: perhaps fewer reach it
+            const float lowest = fmaxf(floor, -FLT_MAX);
+            // the columns that reach it: the vectors of a block whose maximum says there are some are read again,
+            // spread over the threads
+            if (ce < V && xe >= lowest) sh_list[atomicAdd(&sh_count, 1u)] = composite(xe, ce);
+            for (uint32_t b = 0; b << block_shift < step_no; ++b) {
+                if (sh_block[b][tid] >= lowest) {
+                    const unsigned pos = atomicAdd(&sh_hits, 1u);
+                    if (pos < static_cast<unsigned>(kHits)) sh_hit[pos] = static_cast<uint16_t>(b * kThreads + tid);
+                }
+            }
+            __syncthreads();
+            const unsigned hits = sh_hits, per_hit = static_cast<unsigned>(U) << block_shift;
+            if (hits > static_cast<unsigned>(kHits)) {
+                if (tid == 0) sh_count = kCap + 1;               // too many to note: gathered from the row instead
+            } else {
+                for (unsigned i = tid; i < hits * per_hit; i += kThreads) {
+                    const unsigned hit = sh_hit[i / per_hit];
+                    const uint32_t j = share.v_lo + ((hit / kThreads) * per_hit + i % per_hit) * kThreads + hit % kThreads;
+                    if (j >= share.v_hi) continue;
+                    uint4 v = load_vector(share.vectors + j);
+                    const uint32_t col = share.head + j * VEC;
+                    bias_vector<DTYPE, SCHEME>(v, rs, a.vocab_offset + col, a.bias);
+                    if (!(vector_max<DTYPE>(v) >= lowest)) continue;
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        if (!(element<DTYPE>(v, k) >= lowest)) continue;
+                        const unsigned pos = atomicAdd(&sh_count, 1u);
+                        if (pos < static_cast<unsigned>(kCap)) sh_list[pos] = composite(element<DTYPE>(v, k), col + k);
+                    }
+                }
+            }
+            __syncthreads();
             unsigned n = sh_count;
             bool strict = !(floor > -INFINITY);                  // the list holds what is above the floor, not what equals it
             for (int again = 0; again < 2 && n > static_cast<unsigned>(kCap) && !(again == 1 && strict); ++again) {
@@ -658,36 +716,25 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 __syncthreads();
                 n = sh_count;
             }
-            for (unsigned i = tid; i < need; i += kThreads) sh_top[i] = 0;
-            if (n <= static_cast<unsigned>(kCap)) {
-                const uint64_t least = static_cast<uint64_t>(value_code(floor)) << 32;
+            if (n > static_cast<unsigned>(kCap)) {
+                select_rounds<DTYPE, SCHEME>(a, row, c_lo, c_hi, sh_top, need, sh_rounds);
+            } else {
                 for (unsigned i = tid; i < n; i += kThreads) {
                     const uint64_t mine = sh_list[i];
-                    if (mine >= least) {
-                        const unsigned pos = atomicAdd(&sh_kept, 1u);
-                        if (pos < static_cast<unsigned>(kKeep)) sh_keep[pos] = mine;
+                    const unsigned rank = count_larger(sh_list, n, mine);
+                    if (rank < need) {
+                        if (parts > 1) *cluster.map_shared_rank(&sh_all[part * a.top_n + rank], 0) = mine;
+                        else sh_top[rank] = mine;
                     }
                 }
-                __syncthreads();
-                const unsigned kept = sh_kept;
-                const bool few = kept <= static_cast<unsigned>(kKeep);
-                const uint64_t *list = few ? sh_keep : sh_list;
-                const unsigned count = few ? kept : n;
-                for (unsigned i = tid; i < count; i += kThreads) {
-                    const uint64_t mine = list[i];
-                    const unsigned rank = count_larger(list, count, mine);
-                    if (rank < need) sh_top[rank] = mine;
-                }
-                if (count < need && warp == 0) fill_equal<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, sh_top, count, need);
-            } else {
-                __syncthreads();
-                select_rounds<DTYPE, SCHEME>(a, row, c_lo, c_hi, sh_top, need, sh_keep);
+                if (n < need && warp == 0) fill_equal<DTYPE, SCHEME>(a, row, c_lo, c_hi, floor, sh_top, n, need);
             }
-            __syncthreads();
-            if (tid == 0) sh_count = sh_kept = sh_floor = 0;     // for the next row, whose first barrier comes before any use
-            if (parts > 1)
-                for (unsigned i = tid; i < static_cast<unsigned>(a.top_n); i += kThreads)
+            if (parts > 1) {                                     // what is not there yet, and nothing for the rest
+                const unsigned there = n > static_cast<unsigned>(kCap) ? 0u : min(n, need);
+                if (there < need) __syncthreads();
+                for (unsigned i = there + tid; i < static_cast<unsigned>(a.top_n); i += kThreads)
                     *cluster.map_shared_rank(&sh_all[part * a.top_n + i], 0) = i < need ? sh_top[i] : 0;
+            }
         }
         if (parts > 1) cluster.sync();                           // everything has arrived in CTA 0
         else if (!TOP) __syncthreads();
@@ -703,7 +750,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         const bool nothing = m == -INFINITY, ordinary = fabsf(m) < kOrdinary;
         Stats plain = {};
         if (part == 0 && !nothing && !ordinary) plain = sum_plainly<DTYPE, SCHEME>(a, row, 0u, V, m, sh_scratch);
-        if (part == 0 && (parts > 1 || warp == 0)) {             // every warp the same
+        if (part == 0 && warp == kWarps - 1) {
             double z = 0.0, s = 0.0;
             uint32_t above = 0;
             const float ref = ordinary ? m * c : 0.0f;
@@ -725,7 +772,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 // relative to m itself from here on: the terms are 2^((l - m) c) 2^(m c - ref)
                 const double d = static_cast<double>(m) * static_cast<double>(c) - static_cast<double>(ref);
                 s -= d * z;
-                const double f = exp2(-d);
+                const double y = -0.6931471805599453 * d;        // tiny unless m c is huge
+                const double f = fabs(y) < 1e-4 ? 1.0 + y * (1.0 + 0.5 * y) : exp(y);
                 z *= f;
                 s *= f;
             } else {
@@ -733,35 +781,39 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 s = plain.s;
             }
             const double ln_z = log(z);
-            auto logp = [&](float x) -> float {
-                if (z == 0.0) return -INFINITY;                  // every logit is -inf
-                return static_cast<float>((static_cast<double>(x) - static_cast<double>(m)) * a.inv_tau - ln_z);
-            };
-            if (tid == 0) {
-                if (a.out_logprob) a.out_logprob[row] = logp(xt);
-                if (a.out_entropy)
-                    a.out_entropy[row] = z == 0.0 ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
+            if (lane == 0) {
+                const bool empty = z == 0.0;                     // every logit is -inf
+                if (a.out_logprob)
+                    a.out_logprob[row] = empty ? -INFINITY : static_cast<float>((static_cast<double>(xt) - m) * a.inv_tau - ln_z);
+                if (a.out_entropy) a.out_entropy[row] = empty ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
                 if (a.out_rank) a.out_rank[row] = 1 + static_cast<int32_t>(above);
-                const bool bad = z != z;                         // a NaN or +inf among the logits
-                if (a.out_max) a.out_max[row] = bad ? NAN : m;
+                if (a.out_max) a.out_max[row] = z != z ? NAN : m;                    // NaN: a NaN or +inf among the logits
                 if (a.out_sumexp) a.out_sumexp[row] = static_cast<float>(z);
+                if (TOP) {
+                    sh_row[0] = m;
+                    sh_row[1] = ln_z;
+                    sh_row[2] = z;
+                }
             }
-            if constexpr (TOP) {
-                const unsigned n = a.top_n, all = parts > 1 ? n * parts : min(n, V);
-                const uint64_t *list = parts > 1 ? sh_all : sh_top;
-                for (unsigned i = tid; i < all; i += parts > 1 ? kThreads : 32) {
-                    const uint64_t mine = list[i];
-                    if (mine == 0) continue;
-                    unsigned rank = i;
-                    if (parts > 1) rank = count_larger(list, all, mine);
-                    if (rank < n) {
-                        if (a.out_top_ids) a.out_top_ids[row * n + rank] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(mine));
-                        if (a.out_top_logprobs) a.out_top_logprobs[row * n + rank] = logp(composite_value(mine));
+        }
+        if constexpr (TOP) {
+            if (part == 0) {
+                const unsigned n = a.top_n;
+                if (parts > 1) {                                 // the parts' lists into one
+                    for (unsigned i = tid; i < n * parts; i += kThreads) {
+                        const uint64_t mine = sh_all[i];
+                        const unsigned rank = mine ? count_larger(sh_all, n * parts, mine) : n;
+                        if (rank < n) sh_top[rank] = mine;
                     }
                 }
-                for (unsigned i = V + tid; i < n; i += parts > 1 ? kThreads : 32) {   // places no column takes
-                    if (a.out_top_ids) a.out_top_ids[row * n + i] = -1;
-                    if (a.out_top_logprobs) a.out_top_logprobs[row * n + i] = -INFINITY;
+                __syncthreads();
+                if (tid == 0) sh_count = sh_hits = 0;            // for the next row, whose first barrier comes before any use
+                for (unsigned i = tid; i < n; i += kThreads) {
+                    const uint64_t mine = i < V ? sh_top[i] : 0;
+                    const double lp = (static_cast<double>(composite_value(mine)) - sh_row[0]) * a.inv_tau - sh_row[1];
+                    if (a.out_top_ids) a.out_top_ids[row * n + i] = i < V ? static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(mine)) : -1;
+                    if (a.out_top_logprobs)
+                        a.out_top_logprobs[row * n + i] = i >= V || sh_row[2] == 0.0 ? -INFINITY : static_cast<float>(lp);
                 }
             }
         }
@@ -826,36 +878,45 @@ logprob_backward_kernel(const GradArgs a) {
 
     const uint32_t t = a.tokens ? static_cast<uint32_t>(a.tokens[row]) : 0xFFFFFFFFu;
     const bool padded = a.tokens && t >= V;
-    GradRow r = {0.0f, a.c, 0.0f, 0.0f, 0.0f, 0xFFFFFFFFu};
-    bool zero = padded;
-    if (!padded) {
-        const double z = a.sumexp[row];
-        if (z == 0.0) {                                  // every logit is -inf: nothing to move
-            zero = true;
-        } else {
-            const double g = a.grad_logprob ? a.grad_logprob[row] : 0.0;
-            const double h = a.grad_entropy ? a.grad_entropy[row] : 0.0;
-            const double scale = 1.0 / (a.tau * z);
-            r.m = a.max[row];
-            // ln p + H = x ln 2 - ln Z + H
-            r.base = static_cast<float>(scale * (g + (a.grad_entropy ? h * (a.entropy[row] - log(z)) : 0.0)));
-            r.slope = static_cast<float>(scale * h * 0.6931471805599453);
-            r.own = static_cast<float>(g / a.tau);
-            r.t = t;
-        }
-    }
-    RowSeedS<SCHEME> rs;
-    if (!zero) rs.init(a.bias.key, a.ctx + row * a.W, a.W);
-
     const uint32_t first = block * (kGradThreads * kGradVectors) + threadIdx.x;
     uint4 w[kGradVectors];
-    if (!zero) {
+    if (!padded) {
 #pragma unroll
         for (int u = 0; u < kGradVectors; ++u) {
             const uint32_t j = first + u * kGradThreads;
             if (j < layout.nvec) w[u] = load_vector(vectors + j);
         }
     }
+    // the row's factors, in fp64 by one thread while the logits arrive
+    __shared__ GradRow sh_row;
+    __shared__ bool sh_zero;
+    if (threadIdx.x == 0) {
+        GradRow r = {0.0f, a.c, 0.0f, 0.0f, 0.0f, 0xFFFFFFFFu};
+        bool zero = padded;
+        if (!padded) {
+            const double z = a.sumexp[row];
+            if (z == 0.0) {                              // every logit is -inf: nothing to move
+                zero = true;
+            } else {
+                const double g = a.grad_logprob ? a.grad_logprob[row] : 0.0;
+                const double h = a.grad_entropy ? a.grad_entropy[row] : 0.0;
+                const double scale = 1.0 / (a.tau * z);
+                r.m = a.max[row];
+                // ln p + H = x ln 2 - ln Z + H
+                r.base = static_cast<float>(scale * (g + (a.grad_entropy ? h * (a.entropy[row] - log(z)) : 0.0)));
+                r.slope = static_cast<float>(scale * h * 0.6931471805599453);
+                r.own = static_cast<float>(g / a.tau);
+                r.t = t;
+            }
+        }
+        sh_row = r;
+        sh_zero = zero;
+    }
+    RowSeedS<SCHEME> rs;
+    if (!padded) rs.init(a.bias.key, a.ctx + row * a.W, a.W);
+    __syncthreads();
+    const GradRow r = sh_row;
+    const bool zero = sh_zero;
 #pragma unroll
     for (int u = 0; u < kGradVectors; ++u) {
         const uint32_t j = first + u * kGradThreads;
@@ -945,32 +1006,23 @@ BiasParams bias_params(const Common &q) {
     return p;
 }
 
-// CTAs per row.  Without the hash the rows' bytes bound the call: as many CTAs as are resident at once,
-// no more (a row's CTAs should find at least one trip each).  With it the SMs' multipliers do: the
-// fewest CTAs per row whose total comes within 3 % of the best share-out over the SMs.
+// CTAs per row: as many as are resident at once, so that few rows still fill the GPU, but no more than find a
+// trip each, and up to 8 -- larger clusters leave SMs of a GPC unused -- but for a handful of rows.
 int parts_per_row(int64_t B, int64_t nvec, int64_t per_trip, int sm_count, int scheme, int most_parts) {
-    int64_t most = (nvec + per_trip - 1) / per_trip;
-    if (most > most_parts) most = most_parts;
-    if (most < 1) most = 1;
-    if (scheme < 0) {
-        const int64_t fill = static_cast<int64_t>(sm_count) * ctas_per_sm(scheme) / B;
-        return static_cast<int>(fill < 1 ? 1 : fill < most ? fill : most);
-    }
-    int best = 1;
-    double best_eff = 0.0;
-    for (int64_t p = 1; p <= most; ++p) {
-        const int64_t ctas = B * p, waves = (ctas + sm_count - 1) / sm_count;
-        const double eff = static_cast<double>(ctas) / static_cast<double>(waves * sm_count);
-        if (eff > best_eff + 0.03) { best_eff = eff; best = static_cast<int>(p); }
-    }
-    return best;
+    const int64_t slots = static_cast<int64_t>(sm_count) * ctas_per_sm(scheme);
+    int64_t parts = scheme < 0 ? slots / B : (slots + B - 1) / B;
+    const int64_t trips = (nvec + per_trip - 1) / per_trip;
+    const int64_t most = B <= 8 ? most_parts : 8;
+    if (parts > most) parts = most;
+    if (parts > trips) parts = trips;
+    return static_cast<int>(parts < 1 ? 1 : parts);
 }
 
 template <int DTYPE, int SCHEME, bool TOP>
 int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     DeviceInfo di;
     if (int rc = current_device_info(&di)) return rc;
-    using R = Ring<SCHEME, TOP>;
+    using R = Ring<DTYPE, SCHEME, TOP>;
     const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP>;
     // clusters above 8 CTAs and that much shared memory have to be asked for, once per device
     static std::atomic<uint64_t> prepared{0};
