@@ -426,7 +426,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     int64_t src_row = first_row - step;
     const uint4 *src = nullptr;
     int src_left = 0;
-    uint32_t src_groups = 0, src_slot = 0;
+    uint32_t src_groups = 0, src_slot = 0;                       // src_slot: the slot taken from last
     auto next_slot = [](uint32_t s) { return s + R::kGroupBytes == R::kBytes ? 0u : s + R::kGroupBytes; };
     auto copy_checked = [&]() {
         if (src_groups == 0) {                                   // on to the next row that is not padded
@@ -448,10 +448,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         src += kPerTrip;
         src_left -= kPerTrip;
         --src_groups;
-        src_slot = next_slot(src_slot);
     };
-#pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) copy_checked();
+    auto copy_first = [&]() {                                    // fills every slot but the last
+#pragma unroll 1
+        for (src_slot = 0; src_slot < R::kBytes - R::kGroupBytes; src_slot += R::kGroupBytes) copy_checked();
+    };
+    copy_first();
     uint32_t slot = 0;
 
     int64_t row = first_row;                                     // copied before its token was known
@@ -459,9 +461,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     if (parts == 1 && a.tokens && t >= V) {                      // padded: begin again after it
         copy_wait<0>();
         src_row = first_row;
-        src_groups = src_slot = 0;
-#pragma unroll 1
-        for (int i = 0; i < R::kStages - 1; ++i) copy_checked();
+        src_groups = 0;
+        copy_first();
     }
     row = next_real(row, t);
     if (row >= a.B && parts > 1) cluster.barrier_wait();
@@ -505,14 +506,16 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             st.s += s2.x + s2.y;
             z2 = s2 = make_float2(0.0f, 0.0f);
         };
-        auto raise = [&](float m) {                              // a new largest value
+        // The warp's reference: its first trip's largest value, and a larger one only when some value exceeds
+        // that 2^40 times (the sums stay far from overflow), so that the sums are hardly ever moved.
+        float limit = kNoValue;
+        auto raise = [&](float mx) {
+            for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             fold();
-            st.top = m;
-            if (m > kNoValue) {
-                st.move(m * c);
-                least = __fsub_rd(m, far);
-                least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
-            }
+            st.move(mx * c);
+            least = __fsub_rd(mx, far);
+            least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
+            limit = fmaf(far, 0.13333334f, mx);
         };
         // Two columns at a time: in packed operations, or, with the hash, in plain ones, which leave the half
         // of the FMA pipe that multiplies integers to the hash.
@@ -548,7 +551,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             const uint32_t col0 = share.head + j0 * VEC;
             bias_vectors<DTYPE, SCHEME, U>(w, rs, a.vocab_offset + col0, kThreads * VEC, a.bias);
             const float mx = largest_of<DTYPE, U>(w);
-            if (mx > st.top) raise(mx);
+            st.top = fmaxf(st.top, mx);
+            if (__any_sync(0xffffffffu, mx > limit)) raise(mx);
             if constexpr (TOP) {
                 block_top = fmaxf(block_top, mx);
                 if ((step_no + 1) >> block_shift != step_no >> block_shift) {
@@ -572,28 +576,32 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 }
             }
             if (mx >= bar) {                                     // some column may rank before the token
+                if (t - col0 < static_cast<uint32_t>(((U - 1) * kThreads + 1) * VEC)) {   // the token may be among them
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const uint32_t col = col0 + u * (kThreads * VEC);
-                    if (t - col < static_cast<uint32_t>(VEC)) {  // the token's own vector
+                    for (int u = 0; u < U; ++u) {
+                        const uint32_t col = col0 + u * (kThreads * VEC);
 #pragma unroll
                         for (int i = 0; i < VEC; ++i) {
                             const float x = element<DTYPE>(w[u], i);
                             if (x > bar || (x == bar && col + i < t)) count += 1.0f;
                         }
-                    } else if constexpr (DTYPE == SBW_DTYPE_F32) {
-                        const float limit = col < t ? below : bar;
+                    }
+                } else if constexpr (DTYPE == SBW_DTYPE_F32) {
+                    const float over = col0 < t ? below : bar;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
 #pragma unroll
                         for (int i = 0; i < VEC; ++i)
-                            if (element<DTYPE>(w[u], i) > limit) count += 1.0f;
-                    } else {
-                        const uint32_t limit = col < t ? below2 : bar2;
-                        const __nv_bfloat162 l2 = *reinterpret_cast<const __nv_bfloat162 *>(&limit);
-                        const __nv_bfloat162 *q = reinterpret_cast<const __nv_bfloat162 *>(&w[u]);
-                        const __nv_bfloat162 n = __hadd2(__hadd2(__hgt2(q[0], l2), __hgt2(q[1], l2)),
-                                                         __hadd2(__hgt2(q[2], l2), __hgt2(q[3], l2)));
-                        count += __low2float(n) + __high2float(n);
+                            if (element<DTYPE>(w[u], i) > over) count += 1.0f;
                     }
+                } else {
+                    const uint32_t over = col0 < t ? below2 : bar2;
+                    const __nv_bfloat162 o2 = *reinterpret_cast<const __nv_bfloat162 *>(&over);
+                    const __nv_bfloat162 *q = reinterpret_cast<const __nv_bfloat162 *>(w);
+                    __nv_bfloat162 n = __hgt2(q[0], o2);         // at most 16 a half: exact in bf16
+#pragma unroll
+                    for (int i = 1; i < 4 * U; ++i) n = __hadd2(n, __hgt2(q[i], o2));
+                    count += __low2float(n) + __high2float(n);
                 }
             }
         };
@@ -601,16 +609,16 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
             copy_wait<R::kStages - 2>();
             const uint32_t here = slots + slot;
-            slot = next_slot(slot);
             if constexpr (INSIDE) {
 #pragma unroll
                 for (int u = 0; u < R::kGroup; ++u) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
                 copy_commit();
                 src += kPerTrip;
-                src_slot = next_slot(src_slot);
             } else {
                 copy_checked();
             }
+            src_slot = slot;
+            slot = next_slot(slot);
 #pragma unroll 1
             for (int k = 0; k < R::kSteps; ++k) {
                 if (!INSIDE && j0 - tid >= share.v_hi && k > 0) break;   // the share ends before this step
@@ -632,8 +640,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         while (trip < trips) trip_body(std::false_type{});
         const int64_t row_ahead = next_real(row + step, token_ahead);
 
+        if (__any_sync(0xffffffffu, xe > limit)) raise(xe);
         if (ce < V) {
-            if (xe > st.top) raise(xe);
+            st.top = fmaxf(st.top, xe);
             add_pair(max_nan(xe, least), 0.0f);
             z2.y = s2.y = 0.0f;
             fold();
@@ -646,9 +655,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         if (TOP && (step_no >> block_shift) < kBlocks) sh_block[step_no >> block_shift][tid] = block_top;
         // ---- this warp's sums, to CTA 0 ----
         {
-            for (int d = 16; d > 0; d >>= 1) st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
-            st.move(fmaxf(st.top, kNoValue) * c);
             for (int d = 16; d > 0; d >>= 1) {
+                st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
                 st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
                 st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
             }
