@@ -831,10 +831,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     copy_wait<0>();
 }
 
-// Gradient: no reduction, so a row is cut into blocks of kGradVectors vectors per thread and every
-// block works alone.
-constexpr int kGradThreads = 256;
-constexpr int kGradVectors = 4;
+// Gradient: no reduction, so a row is cut into blocks of kGradVectors vectors per thread and every block works
+// alone.  Without the hash a thread has all its loads in flight at once; with it the vectors are taken one by one
+// (the loop's code, eight hash chains long, then fits the instruction cache) and the next one is loaded
+// while one is hashed.
+constexpr int kGradThreads = 128;
+constexpr int kGradVectors = 8;
 
 struct GradArgs {
     const void *logits;
@@ -856,10 +858,9 @@ struct GradArgs {
 struct GradRow {
     float m, c, base, slope, own;
     uint32_t t;
-    __device__ __forceinline__ float at(float l, uint32_t col) const {
+    __device__ __forceinline__ float at(float l) const {
         const float x = max_nan((l - m) * c, kFar);
-        const float g = -ex2_approx_ftz(x) * fmaf(slope, x, base);
-        return col == t ? g + own : g;
+        return -ex2_approx_ftz(x) * fmaf(slope, x, base);
     }
 };
 
@@ -887,13 +888,13 @@ logprob_backward_kernel(const GradArgs a) {
     const uint32_t t = a.tokens ? static_cast<uint32_t>(a.tokens[row]) : 0xFFFFFFFFu;
     const bool padded = a.tokens && t >= V;
     const uint32_t first = block * (kGradThreads * kGradVectors) + threadIdx.x;
-    uint4 w[kGradVectors];
+    const uint32_t end = min(layout.nvec, (block + 1) * (kGradThreads * kGradVectors));
+    constexpr int kHeld = SCHEME == kSchemeNone ? kGradVectors : 1;
+    uint4 w[kHeld];
     if (!padded) {
 #pragma unroll
-        for (int u = 0; u < kGradVectors; ++u) {
-            const uint32_t j = first + u * kGradThreads;
-            if (j < layout.nvec) w[u] = load_vector(vectors + j);
-        }
+        for (int u = 0; u < kHeld; ++u)
+            if (first + u * kGradThreads < end) w[u] = load_vector(vectors + first + u * kGradThreads);
     }
     // the row's factors, in fp64 by one thread while the logits arrive
     __shared__ GradRow sh_row;
@@ -925,19 +926,21 @@ logprob_backward_kernel(const GradArgs a) {
     __syncthreads();
     const GradRow r = sh_row;
     const bool zero = sh_zero;
-#pragma unroll
-    for (int u = 0; u < kGradVectors; ++u) {
-        const uint32_t j = first + u * kGradThreads;
-        if (j >= layout.nvec) break;
+    auto emit = [&](uint4 v, uint32_t j) {               // the gradient of vector j
         const uint32_t col = layout.head + j * VEC;
         float g[VEC];
         if (zero) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) g[i] = 0.0f;
         } else {
-            bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col, a.bias);
+            bias_vector<DTYPE, SCHEME>(v, rs, a.vocab_offset + col, a.bias);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) g[i] = r.at(element<DTYPE>(w[u], i), col + i);
+            for (int i = 0; i < VEC; ++i) g[i] = r.at(element<DTYPE>(v, i));
+            if (r.t - col < static_cast<uint32_t>(VEC)) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (col + i == r.t) g[i] += r.own;
+            }
         }
         if (same_phase) {
             uint4 o;
@@ -952,10 +955,22 @@ logprob_backward_kernel(const GradArgs a) {
                     e[i / 2] = *reinterpret_cast<const uint32_t *>(&p);
                 }
             }
-            reinterpret_cast<uint4 *>(out_vectors)[j] = o;
+            __stcs(reinterpret_cast<uint4 *>(out_vectors) + j, o);   // not read again here: leave L2 to the loads
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) store_one<DTYPE>(out_ptr, col + i, g[i]);
+        }
+    };
+    if constexpr (SCHEME == kSchemeNone) {
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u)
+            if (first + u * kGradThreads < end) emit(w[u], first + u * kGradThreads);
+    } else {
+#pragma unroll 1
+        for (uint32_t j = first; j < end; j += kGradThreads) {
+            const uint4 v = w[0];
+            if (!padded && j + kGradThreads < end) w[0] = load_vector(vectors + j + kGradThreads);
+            emit(v, j);
         }
     }
     if (block == 0) {                                    // ragged ends
@@ -963,8 +978,11 @@ logprob_backward_kernel(const GradArgs a) {
         uint32_t col = V;
         if (threadIdx.x < layout.head) col = threadIdx.x;
         else if (threadIdx.x >= 32 && threadIdx.x - 32 < V - first_tail) col = first_tail + threadIdx.x - 32;
-        if (col < V)
-            store_one<DTYPE>(out_ptr, col, zero ? 0.0f : r.at(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias), col));
+        if (col < V) {
+            float g = zero ? 0.0f : r.at(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias));
+            if (!zero && col == r.t) g += r.own;
+            store_one<DTYPE>(out_ptr, col, g);
+        }
     }
 }
 
