@@ -46,7 +46,8 @@ struct LogprobArgs {
     uint32_t vocab_offset;
     BiasParams bias;
     double inv_tau;
-    float c;               // log2(e) / tau
+    float c;               // log2(e) / tau, rounded
+    double c_off;          // ln 2 times the relative error of that rounding
     const int32_t *tokens; // nullable
     int top_n;
     float *out_logprob, *out_entropy;
@@ -498,7 +499,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         Stats st = {kNoValue * c, 0.0f, 0.0f, -INFINITY, 0u};
         float least = kNoValue;                                  // values below count as this
         [[maybe_unused]] uint32_t least2 = both_halves(kNoValue);
-        float count = 0.0f;                                      // columns that rank before the token
+        uint32_t count = 0;                                      // columns that rank before the token
         [[maybe_unused]] float block_top = -INFINITY;            // largest value of the block of steps
         float2 z2 = {0.0f, 0.0f}, s2 = {0.0f, 0.0f};             // partial sums of the trip
         auto fold = [&]() {
@@ -583,7 +584,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
 #pragma unroll
                         for (int i = 0; i < VEC; ++i) {
                             const float x = element<DTYPE>(w[u], i);
-                            if (x > bar || (x == bar && col + i < t)) count += 1.0f;
+                            if (x > bar || (x == bar && col + i < t)) count += 1u;
                         }
                     }
                 } else if constexpr (DTYPE == SBW_DTYPE_F32) {
@@ -592,16 +593,19 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                     for (int u = 0; u < U; ++u) {
 #pragma unroll
                         for (int i = 0; i < VEC; ++i)
-                            if (element<DTYPE>(w[u], i) > over) count += 1.0f;
+                            if (element<DTYPE>(w[u], i) > over) count += 1u;
                     }
                 } else {
                     const uint32_t over = col0 < t ? below2 : bar2;
                     const __nv_bfloat162 o2 = *reinterpret_cast<const __nv_bfloat162 *>(&over);
                     const __nv_bfloat162 *q = reinterpret_cast<const __nv_bfloat162 *>(w);
-                    __nv_bfloat162 n = __hgt2(q[0], o2);         // at most 16 a half: exact in bf16
+                    // masks of 0xffff per half added up as words: -L in the low half after L hits there, and
+                    // L - H less that borrow in the high one after H hits
+                    uint32_t masks = 0;
 #pragma unroll
-                    for (int i = 1; i < 4 * U; ++i) n = __hadd2(n, __hgt2(q[i], o2));
-                    count += __low2float(n) + __high2float(n);
+                    for (int i = 0; i < 4 * U; ++i) masks += __hgt2_mask(q[i], o2);
+                    const uint32_t low = (0u - masks) & 0xffffu;
+                    count += (low + low - ((masks + low) >> 16)) & 0xffffu;
                 }
             }
         };
@@ -646,9 +650,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             add_pair(max_nan(xe, least), 0.0f);
             z2.y = s2.y = 0.0f;
             fold();
-            if (xe > bar || (xe == bar && ce < t)) count += 1.0f;
+            if (xe > bar || (xe == bar && ce < t)) count += 1u;
         }
-        st.above = static_cast<uint32_t>(count);
+        st.above = count;
         if (t_nothing) st.above = count_above_nothing<DTYPE, SCHEME>(a, row, c_lo, c_hi, t);
 
         [[maybe_unused]] const float largest = st.top;           // of the thread's columns
@@ -788,6 +792,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 z = plain.z;
                 s = plain.s;
             }
+            z -= a.c_off * s;                                    // c was rounded: to first order, 2^(x off) = 1 + x off ln 2
             const double ln_z = log(z);
             if (lane == 0) {
                 const bool empty = z == 0.0;                     // every logit is -inf
@@ -1141,7 +1146,9 @@ extern "C" int sbw_token_logprobs(const void *logits, int dtype, int64_t B, int6
     a.vocab_offset = static_cast<uint32_t>(vocab_offset);
     a.bias = bias_params(q);
     a.inv_tau = 1.0 / static_cast<double>(temperature);
-    a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
+    const double c = 1.4426950408889634 / static_cast<double>(temperature);
+    a.c = static_cast<float>(c);
+    a.c_off = 0.6931471805599453 * (static_cast<double>(a.c) / c - 1.0);
     a.tokens = tokens;
     a.top_n = static_cast<int>(top_n);
     a.out_logprob = out_logprob;
