@@ -544,20 +544,22 @@ weighted_wide_kernel(const WeightedArgs a) {
         for (int w = 1; w < nwarps; ++w) total.add(sh_warp[w]);
         sh_part = total;
     }
-    cluster.sync();
+    if (parts > 1) cluster.sync();
     if (part == 0 && threadIdx.x == 0) {
         WeightSums total = sh_part;
         for (int r = 1; r < parts; ++r) total.add(*cluster.map_shared_rank(&sh_part, r));
         write_weighted(a, seq, total);
     }
-    cluster.sync();                                                   // the sums have been read
+    if (parts > 1) cluster.sync();                                    // the sums have been read
 }
 
 template <int SCHEME>
 cudaError_t launch_weighted(const WeightedArgs &a, int sm_count, cudaStream_t s) {
-    if (const int wide = wide_threads(a.d.N, sm_count)) {
-        // a cluster per sequence while sequences are long enough to keep its CTAs' warps in trips
+    if (int wide = wide_threads(a.d.N, sm_count)) {
+        // no more warps than a text of mean length has trips (1000 texts of 544 tokens: 128 threads, one wave of
+        // CTAs, 7.8 us; 256 threads 8.6 us), and a cluster per sequence while its CTAs' warps all find trips
         const int64_t mean = a.d.total_tokens / a.d.N;
+        while (wide > 64 && mean <= static_cast<int64_t>(wide) * kDetectIlp * 5 / 8) wide /= 2;
         int parts = 1;
         while (parts < 8 && a.d.N * parts * 2 <= sm_count && mean > static_cast<int64_t>(parts) * 32 * 32 * kDetectIlp) parts *= 2;
         cudaLaunchConfig_t cfg = {};
@@ -570,7 +572,7 @@ cudaError_t launch_weighted(const WeightedArgs &a, int sm_count, cudaStream_t s)
         attr[0].val.clusterDim.y = 1;
         attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        cfg.numAttrs = parts > 1 ? 1 : 0;
         switch (a.d.W) {
             case 1: return cudaLaunchKernelEx(&cfg, weighted_wide_kernel<SCHEME, 1>, a);
             case 4: return cudaLaunchKernelEx(&cfg, weighted_wide_kernel<SCHEME, 4>, a);

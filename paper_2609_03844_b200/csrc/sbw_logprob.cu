@@ -689,11 +689,14 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             // the columns that reach it: the vectors of a block whose maximum says there are some are read again,
             // spread over the threads
             if (ce < V && xe >= lowest) sh_list[atomicAdd(&sh_count, 1u)] = composite(xe, ce);
-            for (uint32_t b = 0; b << block_shift < step_no; ++b) {
-                if (sh_block[b][tid] >= lowest) {
-                    const unsigned pos = atomicAdd(&sh_hits, 1u);
-                    if (pos < static_cast<unsigned>(kHits)) sh_hit[pos] = static_cast<uint16_t>(b * kThreads + tid);
-                }
+            unsigned in_blocks = 0;
+#pragma unroll
+            for (uint32_t b = 0; b < kBlocks; ++b)
+                if (b << block_shift < step_no && sh_block[b][tid] >= lowest) in_blocks |= 1u << b;
+            if (in_blocks) {
+                unsigned pos = atomicAdd(&sh_hits, static_cast<unsigned>(__popc(in_blocks)));
+                for (; in_blocks; in_blocks &= in_blocks - 1, ++pos)
+                    if (pos < static_cast<unsigned>(kHits)) sh_hit[pos] = static_cast<uint16_t>((__ffs(in_blocks) - 1) * kThreads + tid);
             }
             __syncthreads();
             const unsigned hits = sh_hits, per_hit = static_cast<unsigned>(U) << block_shift;
@@ -707,12 +710,16 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                     uint4 v = load_vector(share.vectors + j);
                     const uint32_t col = share.head + j * VEC;
                     bias_vector<DTYPE, SCHEME>(v, rs, a.vocab_offset + col, a.bias);
-                    if (!(vector_max<DTYPE>(v) >= lowest)) continue;
+                    unsigned taken = 0;
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) taken |= element<DTYPE>(v, k) >= lowest ? 1u << k : 0u;
+                    if (taken == 0) continue;
+                    unsigned pos = atomicAdd(&sh_count, static_cast<unsigned>(__popc(taken)));
 #pragma unroll
                     for (int k = 0; k < VEC; ++k) {
-                        if (!(element<DTYPE>(v, k) >= lowest)) continue;
-                        const unsigned pos = atomicAdd(&sh_count, 1u);
+                        if (!(taken >> k & 1u)) continue;
                         if (pos < static_cast<unsigned>(kCap)) sh_list[pos] = composite(element<DTYPE>(v, k), col + k);
+                        ++pos;
                     }
                 }
             }
@@ -1076,7 +1083,7 @@ int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
     SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return SBW_OK;
 }
