@@ -396,6 +396,7 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
  *                 alignment take the vectorised path.
  *   ctx_tokens, ctx_width   as for sbw_bias_sample; ctx_tokens may be NULL where delta is 0.
  *   delta         0: no watermark (nothing is hashed).
+ *   temperature   tau, 1e-6 .. 1e6 (SBW_ERR_INVALID_ARG beyond).
  *   tokens        device [B] int32 column indices (0-based within this shard, as sbw_bias_sample
  *                 returns them), or NULL: no out_logprob and no out_rank then.  A token outside
  *                 [0, V) marks a padded row: its logits do not count, its outputs are 0, its

@@ -29,6 +29,11 @@ extern __device__ unsigned int g_sbw_debug[4];   // [0]: bit mask of failed site
 #define SBW_SITE_SAMPLE_OUTPUT 4
 #define SBW_SITE_DETECT_TOKEN 5
 #define SBW_SITE_DETECT_OUTPUT 6
+#define SBW_SITE_LOGPROB_LOAD 7
+#define SBW_SITE_LOGPROB_OUTPUT 8
+#define SBW_SITE_GRAD_LOAD 9
+#define SBW_SITE_GRAD_STORE 10
+#define SBW_SITE_WEIGHT 11
 
 namespace sbw {
 

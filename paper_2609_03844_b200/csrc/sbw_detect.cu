@@ -441,7 +441,8 @@ __device__ __forceinline__ void weigh_trip(const WeightedArgs &a, const int32_t 
 #pragma unroll
     for (int u = 0; u < ILP; ++u) {
         const int t = base + u * 32 + lane;
-        w[u] = !TAIL || static_cast<unsigned>(t) < static_cast<unsigned>(len) ? weights[t] : 0.0f;
+        const bool there = !TAIL || static_cast<unsigned>(t) < static_cast<unsigned>(len);
+        w[u] = there && SBW_CHECKED(t >= 0 && t < len && (weights - a.weights) + t < a.d.total_tokens, SBW_SITE_WEIGHT) ? weights[t] : 0.0f;
     }
     load_trip<SCHEME, WIDTH, TAIL, ILP>(a.d, tok, base, len, lane, v, r, valid);
     philox_word0_n<ILP>(v, r, x, a.d.weyl);

@@ -64,6 +64,14 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 
+// Whether `bytes` bytes at p lie in row `row` of a [B, V] block (bounds-flag build).
+__device__ __forceinline__ bool in_row(const void *base, int64_t ld, int64_t B, int64_t V, int esize, int64_t row, const void *p,
+                                       int bytes) {
+    const char *begin = static_cast<const char *>(base) + row * ld * esize;
+    const char *q = static_cast<const char *>(p);
+    return row >= 0 && row < B && q >= begin && q + bytes <= begin + V * esize;
+}
+
 // ---- where a row's aligned vectors are ----
 // Columns [0, head) come before the first 16-byte boundary, then nvec vectors, then the tail.
 template <int DTYPE>
@@ -444,7 +452,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < R::kGroup; ++u)
-            if (src_left > u * kThreads) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+            if (src_left > u * kThreads &&
+                SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, src_row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
+                copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
         copy_commit();
         src += kPerTrip;
         src_left -= kPerTrip;
@@ -615,7 +625,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             const uint32_t here = slots + slot;
             if constexpr (INSIDE) {
 #pragma unroll
-                for (int u = 0; u < R::kGroup; ++u) copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+                for (int u = 0; u < R::kGroup; ++u)
+                    if (SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
+                        copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
                 copy_commit();
                 src += kPerTrip;
             } else {
@@ -706,7 +718,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 for (unsigned i = tid; i < hits * per_hit; i += kThreads) {
                     const unsigned hit = sh_hit[i / per_hit];
                     const uint32_t j = share.v_lo + ((hit / kThreads) * per_hit + i % per_hit) * kThreads + hit % kThreads;
-                    if (j >= share.v_hi) continue;
+                    if (j >= share.v_hi ||
+                        !SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, share.vectors + j, 16), SBW_SITE_LOGPROB_LOAD))
+                        continue;
                     uint4 v = load_vector(share.vectors + j);
                     const uint32_t col = share.head + j * VEC;
                     bias_vector<DTYPE, SCHEME>(v, rs, a.vocab_offset + col, a.bias);
@@ -803,6 +817,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             const double ln_z = log(z);
             if (lane == 0) {
                 const bool empty = z == 0.0;                     // every logit is -inf
+                (void)SBW_CHECKED(row >= 0 && row < a.B && above < V, SBW_SITE_LOGPROB_OUTPUT);
                 if (a.out_logprob)
                     a.out_logprob[row] = empty ? -INFINITY : static_cast<float>((static_cast<double>(xt) - m) * a.inv_tau - ln_z);
                 if (a.out_entropy) a.out_entropy[row] = empty ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
@@ -906,7 +921,9 @@ logprob_backward_kernel(const GradArgs a) {
     if (!padded) {
 #pragma unroll
         for (int u = 0; u < kHeld; ++u)
-            if (first + u * kGradThreads < end) w[u] = load_vector(vectors + first + u * kGradThreads);
+            if (first + u * kGradThreads < end &&
+                SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, vectors + first + u * kGradThreads, 16), SBW_SITE_GRAD_LOAD))
+                w[u] = load_vector(vectors + first + u * kGradThreads);
     }
     // the row's factors, in fp64 by one thread while the logits arrive
     __shared__ GradRow sh_row;
@@ -939,6 +956,8 @@ logprob_backward_kernel(const GradArgs a) {
     const GradRow r = sh_row;
     const bool zero = sh_zero;
     auto emit = [&](uint4 v, uint32_t j) {               // the gradient of vector j
+        if (!SBW_CHECKED(in_row(a.grad, a.grad_ld, a.B, a.V, Layout::ESIZE, row, out_vectors + static_cast<size_t>(j) * 16, 16), SBW_SITE_GRAD_STORE))
+            return;
         const uint32_t col = layout.head + j * VEC;
         float g[VEC];
         if (zero) {
@@ -981,7 +1000,9 @@ logprob_backward_kernel(const GradArgs a) {
 #pragma unroll 1
         for (uint32_t j = first; j < end; j += kGradThreads) {
             const uint4 v = w[0];
-            if (!padded && j + kGradThreads < end) w[0] = load_vector(vectors + j + kGradThreads);
+            if (!padded && j + kGradThreads < end &&
+                SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, vectors + j + kGradThreads, 16), SBW_SITE_GRAD_LOAD))
+                w[0] = load_vector(vectors + j + kGradThreads);
             emit(v, j);
         }
     }
