@@ -30,11 +30,11 @@ namespace {
 __host__ __device__ constexpr int threads_of(int scheme) { return scheme < 0 ? 256 : 128; }
 __host__ __device__ constexpr int ctas_per_sm(int scheme) { return scheme < 0 ? 3 : 4; }
 constexpr int kCap = 1280;              // candidate list entries
-constexpr int kBlocks = 8;              // blocks of steps whose maxima a thread remembers
+constexpr int kBlocks = 8;              // blocks of trips whose maxima a thread remembers
 constexpr int kHits = 512;              // blocks that reach the bound
 constexpr int kMaxTop = SBW_MAX_TOP_LOGPROBS;
 // CTAs per row at most
-__host__ __device__ constexpr int max_parts(int scheme, bool top) { return top ? 8 : 16; }
+__host__ __device__ constexpr int max_parts(bool top) { return top ? 8 : 16; }
 constexpr float kFar = -300.0f;         // exponents below this give 2^x = 0; keeps 0 * inf out of the sums
 static_assert(kCap >= 16 * kMaxTop + 16, "a share with vectors for fewer groups than alternatives must fit the list");
 
@@ -288,11 +288,9 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
 // Every thread copies its own vectors into its own slots of shared memory, groups of a few vectors
 // some groups ahead (cp.async: no register waits for the data, no barrier, and a thread waits for
 // nothing but its own copies), across row boundaries too, so that the loads go on while a row is finished.
-template <int DTYPE, int SCHEME, bool TOP>
+template <int SCHEME>
 struct Ring {
-    static constexpr int kStep = SCHEME == kSchemeNone ? 4 : 2;              // vectors taken at a time
-    static constexpr int kSteps = SCHEME == kSchemeNone ? 1 : TOP ? 2 : 4;   // steps of a trip; a trip takes one group of copies
-    static constexpr int kGroup = kStep * kSteps;
+    static constexpr int kGroup = SCHEME == kSchemeNone ? 4 : 2;    // vectors of a group; a trip of the loop takes one
     static constexpr int kStages = SCHEME == kSchemeNone ? 3 : 2;
     static constexpr int kThreads = threads_of(SCHEME);
     static constexpr int kGroupBytes = kGroup * kThreads * 16;
@@ -317,7 +315,6 @@ template <int DTYPE>
 struct Share {
     const uint4 *vectors;
     uint32_t head, v_lo, v_hi;
-    __device__ __forceinline__ Share() : vectors(nullptr), head(0), v_lo(0), v_hi(0) {}
     __device__ __forceinline__ Share(const LogprobArgs &a, int64_t row, unsigned part, unsigned parts) {
         const char *row_ptr = static_cast<const char *>(a.logits) + row * a.ld * RowLayout<DTYPE>::ESIZE;
         const RowLayout<DTYPE> layout(row_ptr, static_cast<uint32_t>(a.V));
@@ -377,10 +374,10 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     namespace cg = cooperative_groups;
     using Layout = RowLayout<DTYPE>;
     constexpr int VEC = Layout::VEC;
-    using R = Ring<DTYPE, SCHEME, TOP>;
-    constexpr int U = R::kStep, kPerTrip = R::kGroup * R::kThreads, kThreads = R::kThreads, kWarps = kThreads / 32;
+    using R = Ring<SCHEME>;
+    constexpr int U = R::kGroup, kThreads = R::kThreads, kPerTrip = U * kThreads, kWarps = kThreads / 32;
     extern __shared__ __align__(16) unsigned char sh_ring[];
-    __shared__ Stats sh_warp[2][max_parts(SCHEME, TOP) * kWarps];            // of two rows in turn
+    __shared__ Stats sh_warp[2][max_parts(TOP) * kWarps];            // of two rows in turn
     __shared__ Stats sh_scratch[kWarps];
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
     __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
@@ -389,8 +386,8 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     __shared__ float sh_block[TOP ? kBlocks : 1][kThreads];
     __shared__ __align__(16) uint64_t sh_list[TOP ? kCap : 1];
     __shared__ uint64_t sh_rounds[kWarps];
-    __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];               // this part's alternatives, best first, 0 = none
-    __shared__ __align__(16) uint64_t sh_all[TOP ? kMaxTop * max_parts(SCHEME, TOP) : 1];  // every part's, in CTA 0
+    __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];               // the part's, at the end the row's alternatives in order
+    __shared__ __align__(16) uint64_t sh_all[TOP ? kMaxTop * max_parts(TOP) : 1];  // every part's, in CTA 0
 
     const auto cluster = cg::this_cluster();
     const unsigned parts = cluster.num_blocks(), part = cluster.block_rank();
@@ -451,7 +448,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             }
         }
 #pragma unroll
-        for (int u = 0; u < R::kGroup; ++u)
+        for (int u = 0; u < U; ++u)
             if (src_left > u * kThreads &&
                 SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, src_row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
                 copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
@@ -510,7 +507,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         float least = kNoValue;                                  // values below count as this
         [[maybe_unused]] uint32_t least2 = both_halves(kNoValue);
         uint32_t count = 0;                                      // columns that rank before the token
-        [[maybe_unused]] float block_top = -INFINITY;            // largest value of the block of steps
+        [[maybe_unused]] float block_top = -INFINITY;            // largest value of the block of trips
         float2 z2 = {0.0f, 0.0f}, s2 = {0.0f, 0.0f};             // partial sums of the trip
         auto fold = [&]() {
             st.z += z2.x + z2.y;
@@ -528,46 +525,51 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
             limit = fmaf(far, 0.13333334f, mx);
         };
-        // Two columns at a time: in packed operations, or, with the hash, in plain ones, which leave the half
-        // of the FMA pipe that multiplies integers to the hash.
-        auto add_pair = [&](float l0, float l1) {
-            if constexpr (SCHEME != kSchemeNone) {
-                const float x0 = fmaf(l0, c, -st.ref), x1 = fmaf(l1, c, -st.ref);
-                const float e0 = ex2_approx_ftz(x0), e1 = ex2_approx_ftz(x1);
-                z2 = make_float2(z2.x + e0, z2.y + e1);
-                s2 = make_float2(fmaf(e0, x0, s2.x), fmaf(e1, x1, s2.y));
-                return;
-            }
+        auto add_pair = [&](float l0, float l1) {                // two columns in each operation
             const float2 x = __ffma2_rn(make_float2(l0, l1), make_float2(c, c), make_float2(-st.ref, -st.ref));
             const float2 e = make_float2(ex2_approx_ftz(x.x), ex2_approx_ftz(x.y));
             z2 = __fadd2_rn(z2, e);
             s2 = __ffma2_rn(e, x, s2);
         };
-        uint32_t trip = 0, step_no = 0;
-        uint32_t j0 = share.v_lo + tid;                          // this step's first vector
+        uint32_t trip = 0;
+        uint32_t j0 = share.v_lo + tid;                          // this trip's first vector
         const uint32_t trips = share.template trips<kPerTrip>();
-        int block_shift = 0;                                     // steps of a block: 2^block_shift
+        [[maybe_unused]] int block_shift = 0;                    // trips of a block: 2^block_shift
         if constexpr (TOP) {
-            while (trips * R::kSteps > static_cast<uint32_t>(kBlocks) << block_shift) ++block_shift;
+            while (trips > static_cast<uint32_t>(kBlocks) << block_shift) ++block_shift;
         }
-        auto step_body = [&](const uint32_t from, const auto inside_tag) {
-            constexpr bool INSIDE = decltype(inside_tag)::value;
+        auto trip_body = [&](const auto inside_tag) {
+            constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
+            copy_wait<R::kStages - 2>();
             uint4 w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 constexpr uint32_t kNone = DTYPE == SBW_DTYPE_F32 ? 0xff800000u : 0xff80ff80u;
-                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(from + u * (kThreads * 16))
+                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(slots + slot + u * (kThreads * 16))
                                                                 : make_uint4(kNone, kNone, kNone, kNone);
             }
+            if constexpr (INSIDE) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
+                        copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+                copy_commit();
+                src += kPerTrip;
+            } else {
+                copy_checked();
+            }
+            src_slot = slot;
+            slot = next_slot(slot);
             const uint32_t col0 = share.head + j0 * VEC;
-            bias_vectors<DTYPE, SCHEME, U>(w, rs, a.vocab_offset + col0, kThreads * VEC, a.bias);
+#pragma unroll
+            for (int u = 0; u < U; ++u) bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col0 + u * (kThreads * VEC), a.bias);
             const float mx = largest_of<DTYPE, U>(w);
             st.top = fmaxf(st.top, mx);
             if (__any_sync(0xffffffffu, mx > limit)) raise(mx);
             if constexpr (TOP) {
                 block_top = fmaxf(block_top, mx);
-                if ((step_no + 1) >> block_shift != step_no >> block_shift) {
-                    sh_block[step_no >> block_shift][tid] = block_top;
+                if ((trip + 1) >> block_shift != trip >> block_shift) {
+                    sh_block[trip >> block_shift][tid] = block_top;
                     block_top = -INFINITY;
                 }
             }
@@ -618,32 +620,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                     count += (low + low - ((masks + low) >> 16)) & 0xffffu;
                 }
             }
-        };
-        auto trip_body = [&](const auto inside_tag) {
-            constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
-            copy_wait<R::kStages - 2>();
-            const uint32_t here = slots + slot;
-            if constexpr (INSIDE) {
-#pragma unroll
-                for (int u = 0; u < R::kGroup; ++u)
-                    if (SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
-                        copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
-                copy_commit();
-                src += kPerTrip;
-            } else {
-                copy_checked();
-            }
-            src_slot = slot;
-            slot = next_slot(slot);
-#pragma unroll 1
-            for (int k = 0; k < R::kSteps; ++k) {
-                if (!INSIDE && j0 - tid >= share.v_hi && k > 0) break;   // the share ends before this step
-                step_body(here + k * (U * kThreads * 16), inside_tag);
-                ++step_no;
-                j0 += U * kThreads;
-            }
             fold();                                              // short chains of additions: a trip's, then the trips'
             ++trip;
+            j0 += kPerTrip;
         };
         const uint32_t full = (share.v_hi - share.v_lo) / kPerTrip;
         constexpr uint32_t kAhead = R::kStages - 1;
@@ -668,7 +647,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         if (t_nothing) st.above = count_above_nothing<DTYPE, SCHEME>(a, row, c_lo, c_hi, t);
 
         [[maybe_unused]] const float largest = st.top;           // of the thread's columns
-        if (TOP && (step_no >> block_shift) < kBlocks) sh_block[step_no >> block_shift][tid] = block_top;
+        if (TOP && (trip >> block_shift) < kBlocks) sh_block[trip >> block_shift][tid] = block_top;
         // ---- this warp's sums, to CTA 0 ----
         {
             for (int d = 16; d > 0; d >>= 1) {
@@ -704,7 +683,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             unsigned in_blocks = 0;
 #pragma unroll
             for (uint32_t b = 0; b < kBlocks; ++b)
-                if (b << block_shift < step_no && sh_block[b][tid] >= lowest) in_blocks |= 1u << b;
+                if (b << block_shift < trip && sh_block[b][tid] >= lowest) in_blocks |= 1u << b;
             if (in_blocks) {
                 unsigned pos = atomicAdd(&sh_hits, static_cast<unsigned>(__popc(in_blocks)));
                 for (; in_blocks; in_blocks &= in_blocks - 1, ++pos)
@@ -1081,7 +1060,7 @@ template <int DTYPE, int SCHEME, bool TOP>
 int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     DeviceInfo di;
     if (int rc = current_device_info(&di)) return rc;
-    using R = Ring<DTYPE, SCHEME, TOP>;
+    using R = Ring<SCHEME>;
     const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP>;
     // clusters above 8 CTAs and that much shared memory have to be asked for, once per device
     static std::atomic<uint64_t> prepared{0};
@@ -1091,7 +1070,7 @@ int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
         SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kBytes));
         prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
-    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(SCHEME, TOP));
+    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(TOP));
     const int64_t resident = static_cast<int64_t>(di.sm_count) * ctas_per_sm(SCHEME);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(parts > 1 ? a.B * parts : (a.B < resident ? a.B : resident)));

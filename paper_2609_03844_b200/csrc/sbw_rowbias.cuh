@@ -114,33 +114,6 @@ __device__ __forceinline__ void bias_vector(uint4 &w, const RowSeedS<SCHEME> &rs
     }
 }
 
-// The same on N vectors, vector u at ids vg + u * stride.  Candidate seeds of their own (self-salt) in fp32:
-// two vectors are hashed together, eight dependent chains instead of four.
-template <int DTYPE, int SCHEME, int N>
-__device__ __forceinline__ void bias_vectors(uint4 (&w)[N], const RowSeedS<SCHEME> &rs, uint32_t vg, uint32_t stride,
-                                             const BiasParams &p) {
-    if constexpr (SCHEME == SBW_SCHEME_SELFSALT && DTYPE == SBW_DTYPE_F32 && N % 2 == 0) {
-#pragma unroll
-        for (int u = 0; u < N; u += 2) {
-            uint32_t v[8], x[8];
-            uint64_t r[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = vg + (u + i / 4) * stride + (i & 3);
-                r[i] = seed_selfsalt(p.key, rs.jmin, v[i]);
-            }
-            philox_word0_n<8>(v, r, x, p.weyl);
-            uint32_t *e = reinterpret_cast<uint32_t *>(&w[u]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (x[i] <= p.thr_m1) e[i] = __float_as_uint(__fadd_rn(__uint_as_float(e[i]), p.delta));
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < N; ++u) bias_vector<DTYPE, SCHEME>(w[u], rs, vg + u * stride, p);
-    }
-}
-
 // The same on one logit in memory: column `col` of a row, widened.
 template <int DTYPE, int SCHEME>
 __device__ __forceinline__ float biased_at(const char *row_ptr, uint32_t col, const RowSeedS<SCHEME> &rs, uint32_t vg,
