@@ -65,7 +65,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // Whether `bytes` bytes at p lie in row `row` of a [B, V] block (bounds-flag build).
-__device__ __forceinline__ bool in_row(const void *base, int64_t ld, int64_t B, int64_t V, int esize, int64_t row, const void *p,
+[[maybe_unused]] __device__ __forceinline__ bool in_row(const void *base, int64_t ld, int64_t B, int64_t V, int esize, int64_t row, const void *p,
                                        int bytes) {
     const char *begin = static_cast<const char *>(base) + row * ld * esize;
     const char *q = static_cast<const char *>(p);
@@ -296,18 +296,30 @@ struct Ring {
     static constexpr int kGroupBytes = kGroup * kThreads * 16;
     static constexpr int kBytes = kGroupBytes * kStages;
 };
+// Vector OFFSET (in vectors) from both addresses, which the instruction adds itself.
+template <int OFFSET>
 __device__ __forceinline__ void copy_async(uint32_t smem, const uint4 *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(src));
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %2], 16;" ::"r"(smem), "l"(src), "n"(OFFSET * 16));
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N));
 }
+template <int OFFSET>
 __device__ __forceinline__ uint4 load_shared(uint32_t smem) {
     uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem));
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4 + %5];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem), "n"(OFFSET * 16));
     return r;
+}
+// f(0), ..., f(N - 1) with arguments known to the compiler.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<N, I + 1>(f);
+    }
 }
 
 // The share of CTA `part` of `parts` in a row.
@@ -447,11 +459,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
                 src_groups = share.template trips<kPerTrip>();
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (src_left > u * kThreads &&
-                SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, src_row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
-                copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+        const uint32_t to = slots + src_slot;
+        unrolled<U>([&](auto u) {
+            constexpr int kAt = decltype(u)::value * kThreads;
+            if (src_left > kAt && SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, src_row, src + kAt, 16), SBW_SITE_LOGPROB_LOAD))
+                copy_async<kAt>(to, src);
+        });
         copy_commit();
         src += kPerTrip;
         src_left -= kPerTrip;
@@ -514,8 +527,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             st.s += s2.x + s2.y;
             z2 = s2 = make_float2(0.0f, 0.0f);
         };
-        // The warp's reference: its first trip's largest value, and a larger one only when some value exceeds
-        // that 2^40 times (the sums stay far from overflow), so that the sums are hardly ever moved.
+        // The warp's reference: its first trip's largest value, and a larger one only when some value's term is
+        // more than twice that one's, so that the sums are seldom moved.  (A wider margin, 2^40, saves nothing
+        // that can be measured and costs the entropy digits: S is then a difference of larger numbers.)
         float limit = kNoValue;
         auto raise = [&](float mx) {
             for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -523,7 +537,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             st.move(mx * c);
             least = __fsub_rd(mx, far);
             least2 = both_halves(__bfloat162float(__float2bfloat16_rd(least)));
-            limit = fmaf(far, 0.13333334f, mx);
+            limit = fmaf(far, 1.0f / 300.0f, mx);                // one power of two more
         };
         auto add_pair = [&](float l0, float l1) {                // two columns in each operation
             const float2 x = __ffma2_rn(make_float2(l0, l1), make_float2(c, c), make_float2(-st.ref, -st.ref));
@@ -542,17 +556,18 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             constexpr bool INSIDE = decltype(inside_tag)::value; // this group and the one to copy now are full, of this row
             copy_wait<R::kStages - 2>();
             uint4 w[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
+            const uint32_t at = slots + slot, to = slots + src_slot;
+            unrolled<U>([&](auto u) {
+                constexpr int kAt = decltype(u)::value * kThreads;
                 constexpr uint32_t kNone = DTYPE == SBW_DTYPE_F32 ? 0xff800000u : 0xff80ff80u;
-                w[u] = INSIDE || j0 + u * kThreads < share.v_hi ? load_shared(slots + slot + u * (kThreads * 16))
-                                                                : make_uint4(kNone, kNone, kNone, kNone);
-            }
+                w[decltype(u)::value] = INSIDE || j0 + kAt < share.v_hi ? load_shared<kAt>(at) : make_uint4(kNone, kNone, kNone, kNone);
+            });
             if constexpr (INSIDE) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, src + u * kThreads, 16), SBW_SITE_LOGPROB_LOAD))
-                        copy_async(slots + src_slot + u * (kThreads * 16), src + u * kThreads);
+                unrolled<U>([&](auto u) {
+                    constexpr int kAt = decltype(u)::value * kThreads;
+                    if (SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, src + kAt, 16), SBW_SITE_LOGPROB_LOAD))
+                        copy_async<kAt>(to, src);
+                });
                 copy_commit();
                 src += kPerTrip;
             } else {
