@@ -10,6 +10,15 @@
 //     log p_v = (l_v - m)/tau - ln Z            H = ln Z - ln 2 * S/Z.
 // The gradient needs no reduction at all: with the saved m, Z and H,
 //     dl_v = 1/tau [ g (1[v = t] - p_v) - h p_v (ln p_v + H) ].
+//
+// What bounds them (B200, device time in graph replay).  Plain logits: memory -- 4096 x 128256 bf16 are
+// read in 190 us, 5.5 TB/s or 84 % of the measured copy rate; with the exponentials taken out the same loads run
+// at that rate, with them the SFU is busy 64 % and the issue slots 62 % of the time (8 instructions a logit, one
+// an exponential).  Watermarked logits: the 32x32->64 multiplies of the hash -- 128256 x 592 bf16 368 Gelem/s,
+// 151936 x 592 fp32 self-salt 238 Gelem/s, 0.8 of what the bias kernel reaches; 64 rows on 148 SMs lose another seventh to whole CTAs.
+// A handful of rows: latency -- one row of 128256 with 20 alternatives 8.7 us, of which the last 4.4 us are the
+// short dependent phases after the row's last byte (bound, hits, second look, ranking, merge).  The gradient:
+// memory -- 2048 x 128256 bf16 in 163 us, 98 % of the measured copy rate; watermarked 350 Gelem/s.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -24,9 +33,10 @@
 namespace sbw {
 namespace {
 
-// CTA size.  Without the hash three CTAs of 256 threads per SM (80 registers).  With it (128 registers) four of
-// 128: the same 16 warps as the other hashing kernels, in smaller pieces, so that a call's CTAs share the
-// SMs out more evenly.
+// CTA size.  Without the hash three CTAs of 256 threads per SM (80 registers; 4096 x 128256 bf16: 193 us, four at
+// 64 registers 202, two of 384 threads 206, one of 512 219).  With it (128 registers) four of 128: the same 16
+// warps as the other hashing kernels, in smaller pieces, so that a call's CTAs share the SMs out more
+// evenly (64 x 128256 watermarked: 34 us, two of 256 threads 43).
 __host__ __device__ constexpr int threads_of(int scheme) { return scheme < 0 ? 256 : 128; }
 __host__ __device__ constexpr int ctas_per_sm(int scheme) { return scheme < 0 ? 3 : 4; }
 constexpr int kCap = 1280;              // candidate list entries
@@ -288,6 +298,9 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
 // Every thread copies its own vectors into its own slots of shared memory, groups of a few vectors
 // some groups ahead (cp.async: no register waits for the data, no barrier, and a thread waits for
 // nothing but its own copies), across row boundaries too, so that the loads go on while a row is finished.
+// Three groups of four vectors: 96 KB in flight per SM.  (Four groups: no difference; six or eight vectors a
+// group in two groups: 205 us where this takes 193; loads into registers a trip ahead: 231 us where the ring took
+// 224.)
 template <int SCHEME>
 struct Ring {
     static constexpr int kGroup = SCHEME == kSchemeNone ? 4 : 2;    // vectors of a group; a trip of the loop takes one
@@ -379,7 +392,15 @@ __device__ __forceinline__ unsigned count_larger(const uint64_t *list, unsigned 
 // One CTA per row for large batches (the CTAs go on from row to row), a cluster of up to 16 CTAs per
 // row for small ones: each CTA takes a share of the row's vectors and leaves its sums and
 // alternatives in the shared memory of CTA 0, which merges them.  No workspace, no atomics outside a CTA,
-// one launch.
+// one launch.  (One row, no alternatives: 1 CTA 18.9 us, 8 CTAs 6.3, 16 CTAs 5.3.)
+//
+// Alternatives.  In the pass a thread only remembers the largest value of each of eight blocks of trips.  At
+// the end of the row the top_n-th largest of 32, 64 or 128 maxima of disjoint column sets bounds the alternatives from below
+// (some 24 columns reach it for top_n = 20), the blocks whose maximum reaches it are read again, spread over the
+// threads, and the columns found are ranked by counting.  (Collecting candidates during the pass against a bound
+// from its first trip, tightened later, cost 15 instructions a logit with the hash and 1200 cycles a trip in a
+// single row.)  Rows of many equal values overflow the list: it is gathered again from the row, then without
+// the bound itself, then by rounds of "largest below the last one".
 template <int DTYPE, int SCHEME, bool TOP>
 __global__ void __launch_bounds__(threads_of(SCHEME), ctas_per_sm(SCHEME))
 logprob_kernel(const __grid_constant__ LogprobArgs a) {
