@@ -58,6 +58,7 @@ struct LogprobArgs {
     double inv_tau;
     float c;               // log2(e) / tau, rounded
     double c_off;          // ln 2 times the relative error of that rounding
+    float huge;            // ordinary values end here; a bf16 value
     const int32_t *tokens; // nullable
     int top_n;
     float *out_logprob, *out_entropy;
@@ -122,10 +123,14 @@ struct Stats {
         ref = to;
     }
 };
-// Columns below m - 300 / c count as that (2^-300 = 0), a thread that has met no ordinary value has the
-// reference of -2^100, and rows whose largest value is not within +-2^90 are summed again by
-// sum_plainly: with temperatures within 1e-6 .. 1e6 nothing overflows and no 0 * inf arises.
-constexpr float kNoValue = -0x1p100f, kOrdinary = 0x1p90f;
+// Columns below m - 300 / c count as that (2^-300 = 0).  A reference is m c rounded, so the largest column's
+// exponent is that rounding and not 0: up to 1 for |m c| < 2^25, but 2^(m c - ref) would overflow from 2^31 on
+// (masks of -1e10), and S lose its digits before that.  So 2^25 / c is where ordinary values end
+// (LogprobArgs::huge): rows whose largest value is not within +-huge are summed again by sum_plainly, and what lies
+// below -2 huge -- far below any largest value that counts -- is taken as that, which is also the reference of a
+// warp that has met nothing greater.  With temperatures within 1e-6 .. 1e6 nothing overflows then and no
+// 0 * inf arises.
+constexpr double kOrdinary = 0x1p25;
 
 // Largest value of a vector, NaN dropped.
 template <int DTYPE>
@@ -537,9 +542,10 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
 
         const float below = value_below<DTYPE>(bar);             // equal ones before the token are greater than that
         const uint32_t bar2 = both_halves(bar), below2 = both_halves(below);
-        Stats st = {kNoValue * c, 0.0f, 0.0f, -INFINITY, 0u};
-        float least = kNoValue;                                  // values below count as this
-        [[maybe_unused]] uint32_t least2 = both_halves(kNoValue);
+        const float lowest = -2.0f * a.huge;
+        Stats st = {lowest * c, 0.0f, 0.0f, -INFINITY, 0u};
+        float least = lowest;                                    // values below count as this
+        [[maybe_unused]] uint32_t least2 = both_halves(lowest);
         uint32_t count = 0;                                      // columns that rank before the token
         [[maybe_unused]] float block_top = -INFINITY;            // largest value of the block of trips
         float2 z2 = {0.0f, 0.0f}, s2 = {0.0f, 0.0f};             // partial sums of the trip
@@ -551,7 +557,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         // The warp's reference: its first trip's largest value, and a larger one only when some value's term is
         // more than twice that one's, so that the sums are seldom moved.  (A wider margin, 2^40, saves nothing
         // that can be measured and costs the entropy digits: S is then a difference of larger numbers.)
-        float limit = kNoValue;
+        float limit = lowest;
         auto raise = [&](float mx) {
             for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             fold();
@@ -795,7 +801,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             for (unsigned i = lane; i < n_sums; i += 32) m = fmaxf(m, sums[i].top);
             for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         }
-        const bool nothing = m == -INFINITY, ordinary = fabsf(m) < kOrdinary;
+        const bool nothing = m == -INFINITY, ordinary = fabsf(m) < a.huge;
         Stats plain = {};
         if (part == 0 && !nothing && !ordinary) plain = sum_plainly<DTYPE, SCHEME>(a, row, 0u, V, m, sh_scratch);
         if (part == 0 && warp == kWarps - 1) {
@@ -1192,6 +1198,7 @@ extern "C" int sbw_token_logprobs(const void *logits, int dtype, int64_t B, int6
     const double c = 1.4426950408889634 / static_cast<double>(temperature);
     a.c = static_cast<float>(c);
     a.c_off = 0.6931471805599453 * (static_cast<double>(a.c) / c - 1.0);
+    a.huge = __bfloat162float(__float2bfloat16_rz(static_cast<float>(kOrdinary / c)));
     a.tokens = tokens;
     a.top_n = static_cast<int>(top_n);
     a.out_logprob = out_logprob;

@@ -173,6 +173,29 @@ def test_masks_and_special_values(oracle, dtype, B):
             raise AssertionError(f"watermarked, {name}: {e}") from e
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tau", [1e-3, 0.3, 1.0, 5.0])
+def test_rows_and_masks_of_any_magnitude(oracle, dtype, tau):
+    """2^(l c - round(m c)) leaves the exponent range when m c is large, whether the row's own largest value is that
+    large or only the largest one that some warp meets (a run of masked columns)."""
+    dev = require_gpu()
+    tau = float(np.float32(tau))
+    for V, B in ((300, 3), (9001, 12), (5003, 700)):
+        base = inputs.logits_normal(B, V, 3.0, F32, seed=V, device=dev)
+        t = tokens_of(B, V, 3, dev)
+        power = torch.arange(B, device=dev)[:, None] % 29 + 3.0          # a magnitude from 1e3 to 1e31 a row
+        for sign in (1.0, -1.0):
+            check(oracle, (sign * base.abs() * 10.0 ** power).to(dtype), t, tau, 9)
+            level = torch.full_like(base, sign) * 10.0 ** power          # equal values: entropy ln V
+            check(oracle, level.to(dtype), t, tau)
+            check(oracle, (level * (1 + base.abs() / 2048)).to(dtype), t, tau)
+        masked = base.clone()
+        masked[:, V // 2:] = (-(10.0 ** power)).expand(B, V - V // 2)
+        check(oracle, masked.to(dtype), t, tau, 9)
+        masked[:, :V // 2] -= 2.0 ** 25 * tau * 0.6931472                # near where ordinary values end
+        check(oracle, masked.to(dtype), t, tau, 9)
+
+
 def test_padded_rows(oracle):
     dev = require_gpu()
     for B, V in ((1, 5000), (30, 5000), (400, 1001)):
