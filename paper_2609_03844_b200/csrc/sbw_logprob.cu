@@ -304,7 +304,7 @@ __device__ __noinline__ void select_rounds(const LogprobArgs &a, int64_t row, ui
 // some groups ahead (cp.async: no register waits for the data, no barrier, and a thread waits for
 // nothing but its own copies), across row boundaries too, so that the loads go on while a row is finished.
 // Three groups of four vectors: 96 KB in flight per SM.  (Four groups: no difference; six or eight vectors a
-// group in two groups: 205 us where this takes 193; loads into registers a trip ahead: 231 us where the ring took
+// group in two groups: 205 us where this took 193; loads into registers a trip ahead: 231 us where the ring took
 // 224.)
 template <int SCHEME>
 struct Ring {
@@ -398,6 +398,8 @@ __device__ __forceinline__ unsigned count_larger(const uint64_t *list, unsigned 
 // row for small ones: each CTA takes a share of the row's vectors and leaves its sums and
 // alternatives in the shared memory of CTA 0, which merges them.  No workspace, no atomics outside a CTA,
 // one launch.  (One row, no alternatives: 1 CTA 18.9 us, 8 CTAs 6.3, 16 CTAs 5.3.)
+// SPLIT: whether rows are shared out.  Where they are not, everything about parts falls away at compile time: 850
+// instructions per warp and row were more than a fifth of all (4096 rows of 128256 bf16: 190 us with one kernel for both, 181).
 //
 // Alternatives.  In the pass a thread only remembers the largest value of each of eight blocks of trips.  At
 // the end of the row the top_n-th largest of 32, 64 or 128 maxima of disjoint column sets bounds the alternatives from below
@@ -406,7 +408,7 @@ __device__ __forceinline__ unsigned count_larger(const uint64_t *list, unsigned 
 // from its first trip, tightened later, cost 15 instructions a logit with the hash and 1200 cycles a trip in a
 // single row.)  Rows of many equal values overflow the list: it is gathered again from the row, then without
 // the bound itself, then by rounds of "largest below the last one".
-template <int DTYPE, int SCHEME, bool TOP>
+template <int DTYPE, int SCHEME, bool TOP, bool SPLIT>
 __global__ void __launch_bounds__(threads_of(SCHEME), ctas_per_sm(SCHEME))
 logprob_kernel(const __grid_constant__ LogprobArgs a) {
     namespace cg = cooperative_groups;
@@ -414,8 +416,9 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     constexpr int VEC = Layout::VEC;
     using R = Ring<SCHEME>;
     constexpr int U = R::kGroup, kThreads = R::kThreads, kPerTrip = U * kThreads, kWarps = kThreads / 32;
+    constexpr int kMostParts = SPLIT ? max_parts(TOP) : 1;
     extern __shared__ __align__(16) unsigned char sh_ring[];
-    __shared__ Stats sh_warp[2][max_parts(TOP) * kWarps];            // of two rows in turn
+    __shared__ Stats sh_warp[2][kMostParts * kWarps];            // of two rows in turn
     __shared__ Stats sh_scratch[kWarps];
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
     __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
@@ -425,10 +428,10 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     __shared__ __align__(16) uint64_t sh_list[TOP ? kCap : 1];
     __shared__ uint64_t sh_rounds[kWarps];
     __shared__ uint64_t sh_top[TOP ? kMaxTop : 1];               // the part's, at the end the row's alternatives in order
-    __shared__ __align__(16) uint64_t sh_all[TOP ? kMaxTop * max_parts(TOP) : 1];  // every part's, in CTA 0
+    __shared__ __align__(16) uint64_t sh_all[TOP && SPLIT ? kMaxTop * kMostParts : 1];  // every part's, in CTA 0
 
     const auto cluster = cg::this_cluster();
-    const unsigned parts = cluster.num_blocks(), part = cluster.block_rank();
+    const unsigned parts = SPLIT ? cluster.num_blocks() : 1u, part = SPLIT ? cluster.block_rank() : 0u;
     const uint32_t V = static_cast<uint32_t>(a.V);
     const float c = a.c;
     const unsigned tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -1098,24 +1101,20 @@ int parts_per_row(int64_t B, int64_t nvec, int64_t per_trip, int sm_count, int s
     return static_cast<int>(parts < 1 ? 1 : parts);
 }
 
-template <int DTYPE, int SCHEME, bool TOP>
-int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
-    DeviceInfo di;
-    if (int rc = current_device_info(&di)) return rc;
+template <int DTYPE, int SCHEME, bool TOP, bool SPLIT>
+int launch_logprobs(const LogprobArgs &a, int parts, const DeviceInfo &di, cudaStream_t s) {
     using R = Ring<SCHEME>;
-    const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP>;
+    const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP, SPLIT>;
     // clusters above 8 CTAs and that much shared memory have to be asked for, once per device
     static std::atomic<uint64_t> prepared{0};
-    if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
     if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
-        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        if (SPLIT) SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kBytes));
         prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
-    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(TOP));
     const int64_t resident = static_cast<int64_t>(di.sm_count) * ctas_per_sm(SCHEME);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(parts > 1 ? a.B * parts : (a.B < resident ? a.B : resident)));
+    cfg.gridDim = dim3(static_cast<unsigned>(SPLIT ? a.B * parts : (a.B < resident ? a.B : resident)));
     cfg.blockDim = dim3(R::kThreads);
     cfg.dynamicSmemBytes = R::kBytes;
     cfg.stream = s;
@@ -1125,9 +1124,20 @@ int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.numAttrs = SPLIT ? 1 : 0;
     SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return SBW_OK;
+}
+
+template <int DTYPE, int SCHEME, bool TOP>
+int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
+    DeviceInfo di;
+    if (int rc = current_device_info(&di)) return rc;
+    if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
+    using R = Ring<SCHEME>;
+    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(TOP));
+    return parts > 1 ? launch_logprobs<DTYPE, SCHEME, TOP, true>(a, parts, di, s)
+                     : launch_logprobs<DTYPE, SCHEME, TOP, false>(a, parts, di, s);
 }
 
 template <int DTYPE, int SCHEME>
