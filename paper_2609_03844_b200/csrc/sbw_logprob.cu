@@ -207,31 +207,36 @@ struct Columns {
     }
 };
 
+struct RowSums {
+    double z, s;      // as in Stats, relative to the row's largest value
+};
+
 // The sums of columns [lo, hi) for rows with values of any size, by the whole CTA: the largest value
-// first, then differences.  ref is 0 here and z relative to `top`.
+// first, then differences.  One thread adds up V / blockDim terms here, so they are added in fp64 (in fp32
+// 1000 equal terms in a row would be off by as much as 1.5e-5).
 template <int DTYPE, int SCHEME>
-__device__ __noinline__ Stats sum_plainly(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, float top, Stats *scratch) {
+__device__ __noinline__ RowSums sum_plainly(const LogprobArgs &a, int64_t row, uint32_t lo, uint32_t hi, float top, RowSums *scratch) {
     const Columns<DTYPE, SCHEME> x(a, row);
-    Stats st = {0.0f, 0.0f, 0.0f, top, 0u};
+    RowSums sums = {0.0, 0.0};
     for (uint32_t col = lo + threadIdx.x; col < hi; col += blockDim.x) {
         const float d = max_nan((x[col] - top) * a.c, kFar);
-        const float e = ex2_approx_ftz(d);
-        st.z += e;
-        st.s = fmaf(e, d, st.s);
+        const double e = ex2_approx_ftz(d);
+        sums.z += e;
+        sums.s = fma(e, static_cast<double>(d), sums.s);
     }
     for (int d = 16; d > 0; d >>= 1) {
-        st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
-        st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
+        sums.z += __shfl_xor_sync(0xffffffffu, sums.z, d);
+        sums.s += __shfl_xor_sync(0xffffffffu, sums.s, d);
     }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = st;
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = sums;
     __syncthreads();
-    st.z = st.s = 0.0f;
+    sums = {0.0, 0.0};
     for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
-        st.z += scratch[w].z;
-        st.s += scratch[w].s;
+        sums.z += scratch[w].z;
+        sums.s += scratch[w].s;
     }
-    return st;
+    return sums;
 }
 
 // Columns that rank before column t when its value is -inf (or NaN, which counts as that).
@@ -419,7 +424,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     constexpr int kMostParts = SPLIT ? max_parts(TOP) : 1;
     extern __shared__ __align__(16) unsigned char sh_ring[];
     __shared__ Stats sh_warp[2][kMostParts * kWarps];            // of two rows in turn
-    __shared__ Stats sh_scratch[kWarps];
+    __shared__ RowSums sh_scratch[kWarps];
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
     __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
     __shared__ double sh_row[3];                                 // of the row being finished: largest value, ln Z, Z
@@ -805,7 +810,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         }
         const bool nothing = m == -INFINITY, ordinary = fabsf(m) < a.huge;
-        Stats plain = {};
+        RowSums plain = {};
         if (part == 0 && !nothing && !ordinary) plain = sum_plainly<DTYPE, SCHEME>(a, row, 0u, V, m, sh_scratch);
         if (part == 0 && warp == kWarps - 1) {
             double z = 0.0, s = 0.0;
