@@ -407,8 +407,8 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
  *   out_top_ids, out_top_logprobs   device [B, top_n] int32 / float.  Each may be NULL, not all.
  * A row whose logits are all -inf: every log p is -inf, entropy 0, m -inf, Z 0.  A row with a NaN or
  * +inf among its biased logits: logprob, entropy, m, Z and the alternatives' log p are NaN.
- * Statistics are fp32 sums of fp32 exponentials in a chain of at most 48 additions (V <= 2^18, one
- * more per 16384 columns beyond), merged in fp64: log p is within 8e-6 + 2^-21 (H + |log p|) of its exact value,
+ * Statistics are fp32 sums of fp32 exponentials in chains of at most 39 additions, whatever V, joined in
+ * fp64: log p is within 8e-6 + 2^-21 (H + |log p|) of its exact value,
  * the entropy H within 16e-6 (1 + H); a tenth of that is usual.  The
  * order of the sums is fixed by the shape: equal calls give equal bits.  No workspace; calls on
  * different streams may overlap.  V <= 2^31 - 1.

@@ -132,6 +132,27 @@ struct Stats {
 // 0 * inf arises.
 constexpr double kOrdinary = 0x1p25;
 
+// A thread's fp32 sums take in kChain trips; then the warp adds them to its sums in fp64, so that no chain of fp32
+// additions grows with the row: at most 16 in a trip, one for its two halves, kChain trips, the row's ragged end and
+// five across the warp, 39.  (One chain through the row: 2^20 columns with the hash are 1024 trips, and a term that they
+// all repeat was lost to 1.5e-5, one of 2^22 columns to 6e-5.)
+constexpr uint32_t kChain = 16;
+struct WarpSums {
+    double z, s;      // as in Stats
+    float ref;
+    __device__ __forceinline__ void add(const Stats &st) {
+        const double d = static_cast<double>(ref) - static_cast<double>(st.ref);     // never above 0
+        if (d != 0.0) {
+            const double f = exp2(d);
+            s = f * fma(d, z, s);
+            z *= f;
+            ref = st.ref;
+        }
+        z += static_cast<double>(st.z);
+        s += static_cast<double>(st.s);
+    }
+};
+
 // Largest value of a vector, NaN dropped.
 template <int DTYPE>
 __device__ __forceinline__ float vector_max(const uint4 &w) {
@@ -425,6 +446,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     extern __shared__ __align__(16) unsigned char sh_ring[];
     __shared__ Stats sh_warp[2][kMostParts * kWarps];            // of two rows in turn
     __shared__ RowSums sh_scratch[kWarps];
+    __shared__ WarpSums sh_long[kWarps];                         // of the trips before the last kChain
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
     __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
     __shared__ double sh_row[3];                                 // of the row being finished: largest value, ln Z, Z
@@ -674,15 +696,36 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             ++trip;
             j0 += kPerTrip;
         };
+        auto join_warp = [&]() {
+            for (int d = 16; d > 0; d >>= 1) {
+                st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
+                st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
+            }
+        };
+        auto end_chain = [&]() {                                 // every kChain trips, but for the row's last
+            if (trip % kChain != 0 || trip == trips) return;
+            join_warp();
+            if (lane == 0) {
+                if (trip == kChain) sh_long[warp] = {st.z, st.s, st.ref};
+                else sh_long[warp].add(st);
+            }
+            st.z = st.s = 0.0f;
+        };
         const uint32_t full = (share.v_hi - share.v_lo) / kPerTrip;
         constexpr uint32_t kAhead = R::kStages - 1;
         if (full > kAhead) {
             const uint32_t inside = full - kAhead;               // the copies are kAhead groups ahead, in this row
-            while (trip < inside) trip_body(std::true_type{});
+            while (trip < inside) {
+                trip_body(std::true_type{});
+                end_chain();
+            }
             src_left -= static_cast<int>(inside * kPerTrip);
             src_groups -= inside;
         }
-        while (trip < trips) trip_body(std::false_type{});
+        while (trip < trips) {
+            trip_body(std::false_type{});
+            end_chain();
+        }
         const int64_t row_ahead = next_real(row + step, token_ahead);
 
         if (__any_sync(0xffffffffu, xe > limit)) raise(xe);
@@ -700,10 +743,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         if (TOP && (trip >> block_shift) < kBlocks) sh_block[trip >> block_shift][tid] = block_top;
         // ---- this warp's sums, to CTA 0 ----
         {
-            for (int d = 16; d > 0; d >>= 1) {
-                st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
-                st.z += __shfl_xor_sync(0xffffffffu, st.z, d);
-                st.s += __shfl_xor_sync(0xffffffffu, st.s, d);
+            for (int d = 16; d > 0; d >>= 1) st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
+            join_warp();
+            if (lane == 0 && trips > kChain) {
+                sh_long[warp].add(st);
+                st.z = static_cast<float>(sh_long[warp].z);
+                st.s = static_cast<float>(sh_long[warp].s);
             }
             st.above = __reduce_add_sync(0xffffffffu, st.above);
             if (parts > 1) cluster.barrier_wait();               // CTA 0 runs

@@ -53,3 +53,24 @@ def test_rows_beyond_ordinary_values(V, marked):
     for tau in (0.4, 0.48, 0.59, 0.74, 0.9):
         check(dev, F32, V, -24000000.0, 2.0, tau, marked=marked)
         check(dev, F32, V, 24000002.0, 2.0, tau, n=3, marked=marked)
+
+
+@pytest.mark.parametrize("dtype,V,marked", [(F32, 1 << 25, True), (F32, 1 << 27, False), (BF16, 1 << 26, True),
+                                            (BF16, 1 << 28, False)])
+def test_rows_of_thousands_of_trips(dtype, V, marked):
+    """Every thread meets its part of the row in 4096 trips (eight CTAs to a row with alternatives).  One column of a
+    warp's vectors holds the largest value, so that the terms of all others are relative to it."""
+    dev = require_gpu()
+    for step in (2.5, 1.375, 2.1875, 0.71875):
+        check(dev, dtype, V, 1.0, step, 1.0, n=1, marked=marked, column=0, every=128 if dtype == F32 else 256)
+
+
+@pytest.mark.parametrize("column", [0, 1, 70000, 262143])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_largest_value_in_any_trip(dtype, column):
+    """Trips before the largest value are kept with another reference than those after it."""
+    dev = require_gpu()
+    for marked in (False, True):
+        for n in (0, 2):
+            check(dev, dtype, 1 << 18, 1.0, 2.5, 1.0, n=n, marked=marked, column=column)
+            check(dev, dtype, 1 << 18, 1.0, 2.5, 0.25, n=n, marked=marked, column=column)
