@@ -8,11 +8,13 @@
 
 #include "../../include/sbw.h"
 
-// Bounds-flag build (-DSBW_DEBUG, relocatable device code): every global access of the three core
-// kernels is preceded by a check of its row / column / position against the call's sizes.  A
-// failed check records its site in a device-side flag word and the access is skipped -- no trap,
-// no device assert -- and sbw_debug_flags() reads the words back.  It stands in for a memory
-// checker on machines where none can be run; release builds compile the checks away.
+// Bounds-flag build (-DSBW_DEBUG, relocatable device code): the accesses of the bias, sampling and
+// detection kernels to rows, tokens and workspace, and every logit, gradient element and weight that
+// the log-probability, gradient and weighted kernels touch, are preceded by a check of their row /
+// column / position against the call's sizes.  A failed check records its site in a device-side
+// flag word; where the check's value is used the access is skipped too -- no trap, no device
+// assert -- and sbw_debug_flags() reads the words back.  It stands in for a memory checker on
+// machines where none can be run; release builds compile the checks away.
 #ifdef SBW_DEBUG
 extern __device__ unsigned int g_sbw_debug[4];   // [0]: bit mask of failed sites, [1]: failures, [2]: checks passed
 #define SBW_CHECKED(ok, site)                                                            \

@@ -212,19 +212,30 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
     return r;
 }
 
+// One (biased) logit of a row, widened.
+template <int DTYPE, int SCHEME>
+__device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t row, const char *row_ptr, uint32_t col,
+                                          const RowSeedS<SCHEME> &rs) {
+    constexpr int ESIZE = RowLayout<DTYPE>::ESIZE;
+    if (!SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, ESIZE, row, row_ptr + static_cast<size_t>(col) * ESIZE, ESIZE), SBW_SITE_LOGPROB_LOAD))
+        return -INFINITY;
+    return biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias);
+}
+
 // ---- the seldom taken passes over the columns [lo, hi) of a row: plain, one column at a time, out of
 // line so that the common path's registers do not pay for them ----
 template <int DTYPE, int SCHEME>
 struct Columns {
     const LogprobArgs &a;
+    const int64_t row;
     const char *row_ptr;
     RowSeedS<SCHEME> rs;
-    __device__ __forceinline__ Columns(const LogprobArgs &args, int64_t row)
-        : a(args), row_ptr(static_cast<const char *>(args.logits) + row * args.ld * RowLayout<DTYPE>::ESIZE) {
+    __device__ __forceinline__ Columns(const LogprobArgs &args, int64_t row_index)
+        : a(args), row(row_index), row_ptr(static_cast<const char *>(args.logits) + row * args.ld * RowLayout<DTYPE>::ESIZE) {
         rs.init(args.bias.key, args.ctx + row * args.W, args.W);
     }
     __device__ __forceinline__ float operator[](uint32_t col) const {
-        return biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias);
+        return logit_at<DTYPE, SCHEME>(a, row, row_ptr, col, rs);
     }
 };
 
@@ -561,12 +572,12 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         uint32_t ce = V;
         if (part == 0 && tid < share.head) ce = tid;
         else if (part + 1 == parts && tid >= 32 && tid - 32 < V - share.head - nvec * VEC) ce = share.head + nvec * VEC + tid - 32;
-        if (ce < V) xe = biased_at<DTYPE, SCHEME>(row_ptr, ce, rs, a.vocab_offset + ce, a.bias);
+        if (ce < V) xe = logit_at<DTYPE, SCHEME>(a, row, row_ptr, ce, rs);
 
         // the token's own value; its rank counts the greater ones, and the equal ones before it
         const bool ranked = a.tokens != nullptr && a.out_rank != nullptr;
         float xt = INFINITY;
-        if (a.tokens) xt = biased_at<DTYPE, SCHEME>(row_ptr, t, rs, a.vocab_offset + t, a.bias);
+        if (a.tokens) xt = logit_at<DTYPE, SCHEME>(a, row, row_ptr, t, rs);
         const bool t_nothing = ranked && !(xt > -INFINITY);
         const float bar = ranked && !t_nothing ? xt : INFINITY;
 
@@ -891,13 +902,14 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             const double ln_z = log(z);
             if (lane == 0) {
                 const bool empty = z == 0.0;                     // every logit is -inf
-                (void)SBW_CHECKED(row >= 0 && row < a.B && above < V, SBW_SITE_LOGPROB_OUTPUT);
-                if (a.out_logprob)
-                    a.out_logprob[row] = empty ? -INFINITY : static_cast<float>((static_cast<double>(xt) - m) * a.inv_tau - ln_z);
-                if (a.out_entropy) a.out_entropy[row] = empty ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
-                if (a.out_rank) a.out_rank[row] = 1 + static_cast<int32_t>(above);
-                if (a.out_max) a.out_max[row] = z != z ? NAN : m;                    // NaN: a NaN or +inf among the logits
-                if (a.out_sumexp) a.out_sumexp[row] = static_cast<float>(z);
+                if (SBW_CHECKED(row >= 0 && row < a.B && above < V, SBW_SITE_LOGPROB_OUTPUT)) {
+                    if (a.out_logprob)
+                        a.out_logprob[row] = empty ? -INFINITY : static_cast<float>((static_cast<double>(xt) - m) * a.inv_tau - ln_z);
+                    if (a.out_entropy) a.out_entropy[row] = empty ? 0.0f : static_cast<float>(ln_z - 0.6931471805599453 * s / z);
+                    if (a.out_rank) a.out_rank[row] = 1 + static_cast<int32_t>(above);
+                    if (a.out_max) a.out_max[row] = z != z ? NAN : m;                // NaN: a NaN or +inf among the logits
+                    if (a.out_sumexp) a.out_sumexp[row] = static_cast<float>(z);
+                }
                 if (TOP) {
                     sh_row[0] = m;
                     sh_row[1] = ln_z;
@@ -1086,9 +1098,13 @@ logprob_backward_kernel(const GradArgs a) {
         if (threadIdx.x < layout.head) col = threadIdx.x;
         else if (threadIdx.x >= 32 && threadIdx.x - 32 < V - first_tail) col = first_tail + threadIdx.x - 32;
         if (col < V) {
-            float g = zero ? 0.0f : r.at(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias));
+            const size_t at = static_cast<size_t>(col) * Layout::ESIZE;
+            float g = 0.0f;
+            if (!zero && SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, Layout::ESIZE, row, row_ptr + at, Layout::ESIZE), SBW_SITE_GRAD_LOAD))
+                g = r.at(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias));
             if (!zero && col == r.t) g += r.own;
-            store_one<DTYPE>(out_ptr, col, g);
+            if (SBW_CHECKED(in_row(a.grad, a.grad_ld, a.B, a.V, Layout::ESIZE, row, out_ptr + at, Layout::ESIZE), SBW_SITE_GRAD_STORE))
+                store_one<DTYPE>(out_ptr, col, g);
         }
     }
 }
