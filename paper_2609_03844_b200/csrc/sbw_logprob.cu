@@ -135,7 +135,9 @@ constexpr double kOrdinary = 0x1p25;
 // A thread's fp32 sums take in kChain trips; then the warp adds them to its sums in fp64, so that no chain of fp32
 // additions grows with the row: at most 16 in a trip, one for its two halves, kChain trips, the row's ragged end and
 // five across the warp, 39.  (One chain through the row: 2^20 columns with the hash are 1024 trips, and a term that they
-// all repeat was lost to 1.5e-5, one of 2^22 columns to 6e-5.)
+// all repeat was lost to 1.5e-5, one of 2^22 columns to 6e-5.)  Rows whose shares end within kChain trips have kernels
+// without that step (LONG): it costs their loop 2.5 % though it is never taken (4096 x 128256 bf16, sixteen trips: 187 us
+// without it, 191 with it, in turn on one GPU).
 constexpr uint32_t kChain = 16;
 struct WarpSums {
     double z, s;      // as in Stats
@@ -445,7 +447,7 @@ __device__ __forceinline__ unsigned count_larger(const uint64_t *list, unsigned 
 // from its first trip, tightened later, cost 15 instructions a logit with the hash and 1200 cycles a trip in a
 // single row.)  Rows of many equal values overflow the list: it is gathered again from the row, then without
 // the bound itself, then by rounds of "largest below the last one".
-template <int DTYPE, int SCHEME, bool TOP, bool SPLIT>
+template <int DTYPE, int SCHEME, bool TOP, bool SPLIT, bool LONG>
 __global__ void __launch_bounds__(threads_of(SCHEME), ctas_per_sm(SCHEME))
 logprob_kernel(const __grid_constant__ LogprobArgs a) {
     namespace cg = cooperative_groups;
@@ -457,7 +459,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
     extern __shared__ __align__(16) unsigned char sh_ring[];
     __shared__ Stats sh_warp[2][kMostParts * kWarps];            // of two rows in turn
     __shared__ RowSums sh_scratch[kWarps];
-    __shared__ WarpSums sh_long[kWarps];                         // of the trips before the last kChain
+    __shared__ WarpSums sh_long[LONG ? kWarps : 1];              // of the trips before the last kChain
     __shared__ __align__(16) float sh_group[TOP ? 128 : 4];
     __shared__ unsigned sh_floor[kWarps], sh_count, sh_hits;
     __shared__ double sh_row[3];                                 // of the row being finished: largest value, ln Z, Z
@@ -714,7 +716,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
             }
         };
         auto end_chain = [&]() {                                 // every kChain trips, but for the row's last
-            if (trip % kChain != 0 || trip == trips) return;
+            if (!LONG || trip % kChain != 0 || trip == trips) return;
             join_warp();
             if (lane == 0) {
                 if (trip == kChain) sh_long[warp] = {st.z, st.s, st.ref};
@@ -756,7 +758,7 @@ logprob_kernel(const __grid_constant__ LogprobArgs a) {
         {
             for (int d = 16; d > 0; d >>= 1) st.top = fmaxf(st.top, __shfl_xor_sync(0xffffffffu, st.top, d));
             join_warp();
-            if (lane == 0 && trips > kChain) {
+            if (LONG && lane == 0 && trips > kChain) {
                 sh_long[warp].add(st);
                 st.z = static_cast<float>(sh_long[warp].z);
                 st.s = static_cast<float>(sh_long[warp].s);
@@ -1167,10 +1169,10 @@ int parts_per_row(int64_t B, int64_t nvec, int64_t per_trip, int sm_count, int s
     return static_cast<int>(parts < 1 ? 1 : parts);
 }
 
-template <int DTYPE, int SCHEME, bool TOP, bool SPLIT>
+template <int DTYPE, int SCHEME, bool TOP, bool SPLIT, bool LONG>
 int launch_logprobs(const LogprobArgs &a, int parts, const DeviceInfo &di, cudaStream_t s) {
     using R = Ring<SCHEME>;
-    const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP, SPLIT>;
+    const auto kernel = logprob_kernel<DTYPE, SCHEME, TOP, SPLIT, LONG>;
     // clusters above 8 CTAs and that much shared memory have to be asked for, once per device
     static std::atomic<uint64_t> prepared{0};
     if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
@@ -1200,10 +1202,15 @@ int launch_logprobs(const LogprobArgs &a, cudaStream_t s) {
     DeviceInfo di;
     if (int rc = current_device_info(&di)) return rc;
     if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
-    using R = Ring<SCHEME>;
-    const int parts = parts_per_row(a.B, a.V / RowLayout<DTYPE>::VEC, R::kGroup * R::kThreads, di.sm_count, SCHEME, max_parts(TOP));
-    return parts > 1 ? launch_logprobs<DTYPE, SCHEME, TOP, true>(a, parts, di, s)
-                     : launch_logprobs<DTYPE, SCHEME, TOP, false>(a, parts, di, s);
+    constexpr int64_t per_trip = Ring<SCHEME>::kGroup * Ring<SCHEME>::kThreads;
+    const int64_t nvec = a.V / RowLayout<DTYPE>::VEC;            // of a row, at most
+    const int parts = parts_per_row(a.B, nvec, per_trip, di.sm_count, SCHEME, max_parts(TOP));
+    const bool is_long = (nvec + parts - 1) / parts > kChain * per_trip;
+    if (parts > 1)
+        return is_long ? launch_logprobs<DTYPE, SCHEME, TOP, true, true>(a, parts, di, s)
+                       : launch_logprobs<DTYPE, SCHEME, TOP, true, false>(a, parts, di, s);
+    return is_long ? launch_logprobs<DTYPE, SCHEME, TOP, false, true>(a, parts, di, s)
+                   : launch_logprobs<DTYPE, SCHEME, TOP, false, false>(a, parts, di, s);
 }
 
 template <int DTYPE, int SCHEME>
