@@ -393,11 +393,14 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
  * For this order -0 equals +0 and NaN counts as -inf.
  *
  *   logits, dtype, B, V, ld, vocab_offset, key, gamma, scheme   as for sbw_bias_sample; rows of any
- *                 alignment take the vectorised path.
+ *                 alignment take the vectorised path.  vocab_offset only numbers the columns for
+ *                 the hash: the probabilities are those over the V columns given, so a row has to hold
+ *                 its whole vocabulary.  Vocabulary shards are not joined here, as
+ *                 sbw_sample_combine joins them: a shard without the token would take its row for a padded one.
  *   ctx_tokens, ctx_width   as for sbw_bias_sample; ctx_tokens may be NULL where delta is 0.
  *   delta         0: no watermark (nothing is hashed).
  *   temperature   tau, 1e-6 .. 1e6 (SBW_ERR_INVALID_ARG beyond).
- *   tokens        device [B] int32 column indices (0-based within this shard, as sbw_bias_sample
+ *   tokens        device [B] int32 column indices (0-based, vocab_offset not added, as sbw_bias_sample
  *                 returns them), or NULL: no out_logprob and no out_rank then.  A token outside
  *                 [0, V) marks a padded row: its logits do not count, its outputs are 0, its
  *                 alternatives ids -1 with log probability -inf.
@@ -408,10 +411,11 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
  * A row whose logits are all -inf: every log p is -inf, entropy 0, m -inf, Z 0.  A row with a NaN or
  * +inf among its biased logits: logprob, entropy, m, Z and the alternatives' log p are NaN.
  * Statistics are fp32 sums of fp32 exponentials in chains of at most 39 additions, whatever V, joined in
- * fp64: log p is within 8e-6 + 2^-21 (H + |log p|) of its exact value,
- * the entropy H within 16e-6 (1 + H); a tenth of that is usual.  The
- * order of the sums is fixed by the shape: equal calls give equal bits.  No workspace; calls on
- * different streams may overlap.  V <= 2^31 - 1.
+ * fp64: log p is within 8e-6 + 2^-21 (H + |log p|) of its exact value, the entropy H within
+ * 16e-6 (1 + H); a tenth of that is usual.  The order of a row's sums depends on B, V, dtype, the
+ * scheme (or no watermark), whether top_n is 0, the row's address modulo 16 and the device's number of SMs, and on
+ * nothing else: calls that are equal in these give equal bits, others may differ in the last ones.
+ * No workspace; calls on different streams may overlap.  V <= 2^31 - 1.
  *
  * sbw_token_logprobs_backward -- the gradient of those log probabilities and entropies with respect
  * to the logits (straight through the watermark's addition: d l'_v / d l_v = 1):
@@ -423,7 +427,8 @@ int sbw_bias_sample_filtered(const void *logits, int dtype, int64_t B, int64_t V
  *                 where grad_logprob is.
  *   grad_logits   device [B, grad_ld] of `dtype`: every element of columns 0 .. V-1 is written, the
  *                 rest of a row is not; rounded once.  It may be `logits` itself (grad_ld = ld): the gradient then
- *                 takes the logits' place.  Any other overlap of the two is SBW_ERR_INVALID_ARG.
+ *                 takes the logits' place.  Any other overlap of the two is SBW_ERR_INVALID_ARG, and so are
+ *                 rows that lie between each other's with different strides (they are not told apart).
  * Padded rows and rows whose logits are all -inf get zeros; rows with NaN or +inf get NaN.  p_v is an
  * fp32 exponential: relative error below 2^-21 + 2^-22 (m - l'_v) / tau (below 2^-126 it is 0).
  */
@@ -454,7 +459,7 @@ int sbw_token_logprobs_backward(const void *logits, int dtype, int64_t B, int64_
  *   out_z       device [N] double.
  * Other arguments, lengths, offsets and workspace as for sbw_detect
  * (sbw_detect_workspace_bytes(N) where offsets is NULL).  The order of the sums is fixed by N, the
- * lengths and total_tokens: equal calls give equal bits.
+ * lengths, total_tokens and the device's number of SMs: equal calls give equal bits.
  */
 int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32_t *lengths,
                         const int64_t *offsets, int64_t N, int64_t total_tokens, int ctx_width, uint64_t key,

@@ -566,8 +566,9 @@ def sbw_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, temper
     """Log probability, entropy and rank of ``tokens`` (int32 ``[B]``, one per row of ``logits``), the rows'
     softmax statistics and their ``n`` most probable alternatives (``out_top_ids`` int32 and
     ``out_top_logprobs`` float32, both ``[B, n]``).  With ``delta`` the numbers are those of the watermarked
-    logits; ``logits`` itself is not changed.  A token outside ``[0, V)`` marks a padded row.  Outputs are
-    caller-allocated and may be left out; returns ``out_logprob``."""
+    logits; ``logits`` itself is not changed.  A token outside ``[0, V)`` marks a padded row, so rows hold their
+    whole vocabulary, not a shard of it.  Outputs are caller-allocated and may be left out; they have no ``grad_fn``
+    (:func:`sbw_token_logprobs_backward` is the gradient).  Returns ``out_logprob``."""
     B, V, ld = _logits_layout("logits", logits, V)
     dev = logits.get_device()
     n = 0
@@ -599,7 +600,8 @@ def sbw_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor | Non
                                 stream=None) -> torch.Tensor:
     """Gradient of ``sum(grad_logprob * logprob + grad_entropy * entropy)`` with respect to ``logits`` into
     ``grad_logits`` (same type, ``[B, >=V]``; may be ``logits`` itself), from the ``max``, ``sumexp`` and
-    ``entropy`` that :func:`sbw_token_logprobs` gave for the same arguments.  Returns ``grad_logits``."""
+    ``entropy`` that :func:`sbw_token_logprobs` gave for the same arguments.  Autograd does not make this call: a
+    training program does, or an autograd function of its own.  Returns ``grad_logits``."""
     B, V, ld = _logits_layout("logits", logits, V)
     gB, _, grad_ld = _logits_layout("grad_logits", grad_logits, V)
     dev, f32 = logits.get_device(), torch.float32

@@ -12,13 +12,14 @@
 //     dl_v = 1/tau [ g (1[v = t] - p_v) - h p_v (ln p_v + H) ].
 //
 // What bounds them (B200, device time in graph replay).  Plain logits: memory -- 4096 x 128256 bf16 are
-// read in 190 us, 5.5 TB/s or 84 % of the measured copy rate; with the exponentials taken out the same loads run
-// at that rate, with them the SFU is busy 64 % and the issue slots 62 % of the time (8 instructions a logit, one
-// an exponential).  Watermarked logits: the 32x32->64 multiplies of the hash -- 128256 x 592 bf16 368 Gelem/s,
-// 151936 x 592 fp32 self-salt 238 Gelem/s, 0.8 of what the bias kernel reaches; 64 rows on 148 SMs lose another seventh to whole CTAs.
-// A handful of rows: latency -- one row of 128256 with 20 alternatives 8.7 us, of which the last 4.4 us are the
+// read in 181 to 190 us, by the clock that the power cap leaves, 5.5 to 5.8 TB/s or 84 to 89 % of the measured copy rate; with the
+// exponentials taken out the same loads run at that rate, with them the SFU is busy 66 % and the issue slots 62 % of the
+// time (8 instructions a logit, one an exponential).  Watermarked logits: the 32x32->64 multiplies of the hash --
+// 592 x 128256 bf16 380 Gelem/s, 592 x 151936 fp32 self-salt 221 Gelem/s, 0.75 to 0.8 of what the bias kernel reaches; 64
+// rows on 148 SMs lose another seventh to whole CTAs.
+// A handful of rows: latency -- one row of 128256 with 20 alternatives 8.6 us, of which the last 4.4 us are the
 // short dependent phases after the row's last byte (bound, hits, second look, ranking, merge).  The gradient:
-// memory -- 2048 x 128256 bf16 in 163 us, 98 % of the measured copy rate; watermarked 350 Gelem/s.
+// memory -- 2048 x 128256 bf16 in 160 us, the measured copy rate; watermarked 345 Gelem/s, self-salt 230 to 238.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -136,7 +137,7 @@ constexpr double kOrdinary = 0x1p25;
 // additions grows with the row: at most 16 in a trip, one for its two halves, kChain trips, the row's ragged end and
 // five across the warp, 39.  (One chain through the row: 2^20 columns with the hash are 1024 trips, and a term that they
 // all repeat was lost to 1.5e-5, one of 2^22 columns to 6e-5.)  Rows whose shares end within kChain trips have kernels
-// without that step (LONG): it costs their loop 2.5 % though it is never taken (4096 x 128256 bf16, sixteen trips: 187 us
+// without that step (LONG): it costs their loop 2 % though it is never taken (4096 x 128256 bf16, sixteen trips: 187 us
 // without it, 191 with it, in turn on one GPU).
 constexpr uint32_t kChain = 16;
 struct WarpSums {
@@ -1157,8 +1158,10 @@ BiasParams bias_params(const Common &q) {
     return p;
 }
 
-// CTAs per row: as many as are resident at once, so that few rows still fill the GPU, but no more than find a
-// trip each, and up to 8 -- larger clusters leave SMs of a GPC unused -- but for a handful of rows.
+// CTAs per row, so that few rows still fill the GPU: as many as are resident at once, or with the hash the next
+// whole number above that (256 x 151936 fp32 self-salt: 2 CTAs 227 us, 3 218, where 2.3 would be resident; no rule was found
+// in 4 to 8 CTAs: 220, 216, 207, 223, 219); but no more than find a trip each, and up to 8 -- larger clusters leave
+// SMs of a GPC unused -- but for a handful of rows (one row without alternatives: 8 CTAs 6.3 us, 16 CTAs 5.3).
 int parts_per_row(int64_t B, int64_t nvec, int64_t per_trip, int sm_count, int scheme, int most_parts) {
     const int64_t slots = static_cast<int64_t>(sm_count) * ctas_per_sm(scheme);
     int64_t parts = scheme < 0 ? slots / B : (slots + B - 1) / B;
