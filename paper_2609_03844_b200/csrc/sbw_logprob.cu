@@ -219,7 +219,7 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
 template <int DTYPE, int SCHEME>
 __device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t row, const char *row_ptr, uint32_t col,
                                           const RowSeedS<SCHEME> &rs) {
-    constexpr int ESIZE = RowLayout<DTYPE>::ESIZE;
+    [[maybe_unused]] constexpr int ESIZE = RowLayout<DTYPE>::ESIZE;
     if (!SBW_CHECKED(in_row(a.logits, a.ld, a.B, a.V, ESIZE, row, row_ptr + static_cast<size_t>(col) * ESIZE, ESIZE), SBW_SITE_LOGPROB_LOAD))
         return -INFINITY;
     return biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias);

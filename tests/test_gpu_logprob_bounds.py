@@ -3,7 +3,7 @@ vector, whose logits and gradients are all single columns, and the passes of one
 import pytest
 import torch
 
-from paper_2609_03844_b200 import inputs
+from paper_2609_03844_b200 import binding, inputs
 from gpu_util import KEY, require_gpu
 from test_gpu_logprob_owed import _flags, dbg  # noqa: F401
 
@@ -54,3 +54,31 @@ def test_the_passes_of_single_columns(dbg):  # noqa: F811
     mask, failures, passed, _ = _flags(dbg)
     assert mask == 0 and failures == 0 and passed > B * V                      # the row's own pass is a quarter of that
     assert torch.equal(ids.cpu(), torch.arange(5, dtype=torch.int32).expand(B, 5)) and torch.equal(rank, t + 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,delta", [(600, 36007, 2.0), (230, 140009, 0.0), (1, 600011, 2.0)])
+def test_rows_of_more_than_sixteen_trips(dbg, B, V, delta, dtype):  # noqa: F811
+    """No access outside, and the bits of the release build."""
+    dev = require_gpu()
+    x = inputs.logits_normal(B, V, 3.0, dtype, seed=V, device=dev)
+    t = inputs.uniform_tokens((B,), V, 5, dev)
+    t[::4] = -1 if B > 1 else 7
+    ctx = inputs.uniform_tokens((B, 2), V, 6, dev)
+    results = []
+    for L in (dbg, binding.lib()):
+        for scheme in (0, 1):
+            for n in (0, 7):
+                f = [torch.zeros(B, device=dev) for _ in range(4)]
+                rank, ids = torch.zeros(B, dtype=torch.int32, device=dev), torch.zeros((B, 7), dtype=torch.int32, device=dev)
+                _flags(dbg)
+                lp, ent, m, z = (v.data_ptr() for v in f)
+                assert L.sbw_token_logprobs(x.data_ptr(), int(dtype == torch.bfloat16), B, V, V, 0, ctx.data_ptr(), 2, KEY, 0.25,
+                                            delta, scheme, 1.0, t.data_ptr(), n, lp, ent, rank.data_ptr(), m, z,
+                                            ids.data_ptr() if n else None, None, None) == 0
+                torch.cuda.synchronize()
+                results.append([*f, rank, ids])
+                if L is dbg:
+                    mask, failures, passed, _ = _flags(dbg)
+                    assert mask == 0 and failures == 0 and passed > 0
+    assert all(torch.equal(a, b) for p, q in zip(results[:4], results[4:]) for a, b in zip(p, q))
