@@ -466,6 +466,50 @@ int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32
                         double gamma, int scheme, double *out_green, double *out_weight, double *out_weight2,
                         double *out_z, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * sbw_quantize_fp8 -- values to e4m3 (the finite 8-bit format with 4 exponent bits, largest value 448) with
+ * one fp32 scale for each block of 128 columns: the form in which sbw_head_logits takes its operands.
+ * Over the elements of a block, amax the largest magnitude:
+ *     scale = max(amax / 448, 2^-126)      code = e4m3(x / scale)
+ * (both divisions in fp32, the code rounded to nearest even and held within +-448).  x is within half an
+ * e4m3 step of code * scale.  A block that holds a NaN or an infinity comes back with a scale that is none of a
+ * number and as NaN wherever its code times its scale is taken.
+ *   x           device, [R, ld] of `dtype`, R >= 0 rows, K > 0 columns, ld >= K; any alignment of an element
+ *               (rows that start on 16-byte boundaries, and on 8-byte ones in `out`, take the vectorised path).
+ *   block_rows  1: a scale per row and 128 columns (hidden states).  128: a scale per 128 x 128 block (weights).
+ *   out         device, [R, ld_out] bytes, ld_out >= K; columns K .. ld_out - 1 are not written.
+ *   scales      device, [ceil(R / block_rows), ld_scales] float, ld_scales >= ceil(K / 128).
+ * x, out and scales may not overlap.
+ *
+ * sbw_head_logits -- the projection of hidden states to the vocabulary, with the bias of Eq. 1 + Eq. 2 on the
+ * way out (the paper's Section 5.1 speaks of absorbing the watermark into existing steps; this step makes the
+ * logits).  With x and w in e4m3:
+ *     l[b, v] = sum_kb x_scales[b, kb] w_scales[v / 128, kb] sum_{k in block kb} x[b, k] w[v, k]
+ * summed in fp32 (a block's sum on the tensor cores, the blocks in order by fused multiply-add with the product
+ * of the two scales), rounded once to `dtype`; green logits then get delta as in sbw_bias_logits: the result has
+ * the bits of sbw_head_logits with delta 0 followed by sbw_bias_logits.
+ *   x           device, [B, ld_x] e4m3 codes, 16-byte aligned, ld_x >= K a multiple of 16 (any value where B is 1);
+ *               x_scales device [B, ld_x_scales] float, ld_x_scales >= ceil(K / 128).
+ *   w           device, [V, ld_w] e4m3 codes, one row per vocabulary entry, aligned likewise;
+ *               w_scales device [ceil(V / 128), ld_w_scales] float.
+ *   logits      device, [B, ld] of `dtype`; columns 0 .. V-1 of every row are written, the others are not.
+ *               It may not overlap the operands.
+ *   delta       0: the plain product; ctx_tokens may be NULL then (and where delta is 0 in the logits' precision).
+ *   vocab_offset, ctx_tokens, ctx_width, key, gamma, scheme   as for sbw_bias_logits (a shard of the vocabulary is a
+ *               slice of w's rows that starts at a multiple of 128, with its first row's id in vocab_offset).
+ * An e4m3 NaN or a scale that is not finite makes the logits that it enters NaN or infinite.  Equal calls give
+ * equal bits; a row's logits do not depend on the other rows.  The gradient of the hidden states is the same product
+ * with the transposed weights (codes and scales both transposed; blocks of 128 x 128 stay blocks):
+ * d_x = d_l w, with d_l quantized in blocks of one row.
+ * No workspace; calls on different streams may overlap.
+ */
+int sbw_quantize_fp8(const void *x, int dtype, int64_t R, int64_t K, int64_t ld, int64_t block_rows, void *out,
+                     int64_t ld_out, float *scales, int64_t ld_scales, void *stream);
+int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scales, int64_t ld_x_scales, const void *w,
+                    int64_t ld_w, const float *w_scales, int64_t ld_w_scales, int64_t B, int64_t V, int64_t K,
+                    void *logits, int dtype, int64_t ld, int64_t vocab_offset, const int32_t *ctx_tokens,
+                    int ctx_width, uint64_t key, double gamma, float delta, int scheme, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,7 +35,8 @@ EXPORTS = ("sbw_version", "sbw_last_cuda_error", "sbw_bias_logits",
            "sbw_window_z", "sbw_prefix_z", "sbw_detect_unique_workspace_bytes", "sbw_detect_unique",
            "sbw_roc_auc_workspace_bytes", "sbw_roc_auc", "sbw_sample_filtered_workspace_bytes",
            "sbw_bias_sample_filtered", "sbw_roc_auc_batched", "sbw_bias_sample_shard_ids",
-           "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted")
+           "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted", "sbw_quantize_fp8",
+           "sbw_head_logits")
 
 _lib = None
 
@@ -148,6 +149,11 @@ def lib() -> ctypes.CDLL:
         L.sbw_detect_weighted.restype = i32
         L.sbw_detect_weighted.argtypes = [vp, vp, vp, vp, i64, i64, i32, u64, c.c_double, i32, vp, vp, vp, vp, vp,
                                           sz, vp]
+        L.sbw_quantize_fp8.restype = i32
+        L.sbw_quantize_fp8.argtypes = [vp, i32, i64, i64, i64, i64, vp, i64, vp, i64, vp]
+        L.sbw_head_logits.restype = i32
+        L.sbw_head_logits.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, i64, vp, i32, u64,
+                                      c.c_double, c.c_float, i32, vp]
         L.sbw_int_probe.restype = i32
         L.sbw_int_probe.argtypes = [i32, i32, i32, i32, vp, vp, vp]
         atexit.register(_drain_at_exit)
@@ -640,6 +646,58 @@ def sbw_detect_weighted(tokens: torch.Tensor, weights: torch.Tensor, lengths: to
     _launch("sbw_detect_weighted", dev, stream, *given, starts, N, total, ctx_width, key, gamma, scheme, green, weight,
             weight2, z, scratch, ws_bytes)
     return out_z
+
+
+def _operand(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, cols: int, device: int):
+    """(address, row stride) of a ``[rows, cols]`` tensor of ``dtype`` with unit column stride on ``device``."""
+    if t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on cuda:{device}")
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must have shape [{rows}, {cols}], got {list(t.shape)}")
+    if t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+
+
+def sbw_quantize_fp8(x: torch.Tensor, out: torch.Tensor, scales: torch.Tensor, *, block_rows: int = 1, stream=None):
+    """``x`` (``[R, K]``, float32 or bfloat16) as float8_e4m3fn codes ``out`` (``[R, K]``) and one float32 scale per
+    ``block_rows`` x 128 block: ``scales`` is ``[ceil(R / block_rows), ceil(K / 128)]``.  ``block_rows`` 1 is the form of
+    :func:`sbw_head_logits`' hidden states, 128 that of its weights.  Returns ``(out, scales)``."""
+    if not x.is_cuda or x.dim() != 2:
+        raise ValueError("x must be a 2-D CUDA tensor")
+    if block_rows not in (1, 128):
+        raise ValueError(f"block_rows must be 1 or 128, got {block_rows}")
+    (R, K), dev = x.shape, x.get_device()
+    if x.stride(1) != 1 and K > 1:
+        raise ValueError("x must have unit column stride")
+    codes, ld_out = _operand("out", out, torch.float8_e4m3fn, R, K, dev)
+    at, ld_scales = _operand("scales", scales, torch.float32, -(-R // block_rows), -(-K // 128), dev)
+    _launch("sbw_quantize_fp8", dev, stream, x.data_ptr(), _dtype_code(x), R, K, x.stride(0) if R > 1 else max(x.stride(0), K),
+            block_rows, codes, ld_out, at, ld_scales)
+    return out, scales
+
+
+def sbw_head_logits(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
+                    logits: torch.Tensor, *, ctx_tokens: torch.Tensor | None = None, key: int = 0, gamma: float = 0.5,
+                    delta: float = 0.0, scheme: int = SCHEME_CONTEXT, vocab_offset: int = 0, stream=None) -> torch.Tensor:
+    """``logits = x w^T`` for hidden states ``x`` (``[B, K]``) and weights ``w`` (``[V, K]``), both float8_e4m3fn with
+    rows that start on 16-byte boundaries, scaled by ``x_scales`` (``[B, ceil(K / 128)]``) and ``w_scales``
+    (``[ceil(V / 128), ceil(K / 128)]``); with ``delta`` the watermark is added on the way out, with the bits that
+    :func:`sbw_bias_logits` gives.  ``logits`` is float32 or bfloat16, ``[B, >=V]``; columns from ``V`` on are not written.
+    Returns ``logits``."""
+    if not x.is_cuda or x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be 2-D CUDA tensors")
+    (B, K), V, dev = x.shape, w.shape[0], x.get_device()
+    e4m3, blocks = torch.float8_e4m3fn, -(-K // 128)
+    given = (*_operand("x", x, e4m3, B, K, dev), *_operand("x_scales", x_scales, torch.float32, B, blocks, dev),
+             *_operand("w", w, e4m3, V, K, dev), *_operand("w_scales", w_scales, torch.float32, -(-V // 128), blocks, dev))
+    rows, _, ld = _logits_layout("logits", logits, V)
+    if rows != B or logits.get_device() != dev:
+        raise ValueError(f"logits must have {B} rows and be on cuda:{dev}")
+    ctx, W = _watermark(ctx_tokens, B, delta, dev)
+    _launch("sbw_head_logits", dev, stream, *given, B, V, K, logits.data_ptr(), _dtype_code(logits), ld, vocab_offset, ctx,
+            W, key, gamma, delta, scheme)
+    return logits
 
 
 PROBE_KINDS = {"mulwide": (0, 1), "lop3": (1, 1), "iadd3": (2, 1), "imad": (3, 1), "philox": (4, 4),

@@ -36,6 +36,7 @@ extern __device__ unsigned int g_sbw_debug[4];   // [0]: bit mask of failed site
 #define SBW_SITE_GRAD_LOAD 9
 #define SBW_SITE_GRAD_STORE 10
 #define SBW_SITE_WEIGHT 11
+#define SBW_SITE_HEAD_STORE 12
 
 namespace sbw {
 

@@ -1,0 +1,506 @@
+// sbw_head_logits: the projection to the vocabulary on the 5th-generation tensor cores, hidden states and
+// weights in e4m3 with one fp32 scale for each block of 128, and the watermark (Eq. 1 + Eq. 2) in its
+// epilogue.
+//
+//     l[b, v] = sum_kb  xs[b, kb] ws[v / 128, kb]  sum_{k in block kb} x[b, k] w[v, k]
+//
+// Every CTA is persistent and owns an SM: it walks tiles of 128 rows (hidden states) by BN columns
+// (vocabulary).
+//   warp 0       copies 128-byte wide blocks of both operands into a ring of shared-memory stages (TMA)
+//   warp 1       one thread issues tcgen05.mma: the product of one block of 128 goes to one of the
+//                accumulators in tensor memory and starts from zero there
+//   warps 4..11  read that product back, multiply it by the two scales and add it to fp32 sums in
+//                registers: a block's scales are arbitrary fp32 numbers, which the matrix unit cannot
+//                apply itself; row = lane, so that a thread's row has one scale per block
+// The hidden states are the side with 128 rows whatever B is: at small B the weights' bytes bound the
+// call and the matrix unit's time for rows that are not there is hidden behind them.  (With the sides
+// exchanged every thread needs a scale per column and block from shared memory.)
+//
+// Every wait is bounded: one that does not end within kWaitLimit gives up, the rest of the CTA's logits
+// are NaN, and the kernel returns.
+#include <atomic>
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "sbw_common.cuh"
+#include "sbw_hash.cuh"
+#include "sbw_rowbias.cuh"
+
+namespace sbw {
+namespace {
+
+constexpr int kBlock = 128;            // columns of the operands per scale, and bytes per row of a stage
+constexpr int kTileM = 128;
+constexpr int kHeadThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kMaxStages = 16;
+constexpr int kTmemColumns = 512;
+constexpr uint64_t kWaitLimit = 2000000000ull;      // nanoseconds
+constexpr int kStageWords = 32 * 33;                // a warp's staging area for stores: 32 rows of 32 words, padded
+constexpr int kStagingBytes = kEpilogueWarps * kStageWords * 4;
+constexpr int kMaxDynamicBytes = 227 * 1024 - 1024;  // what a CTA can have less the barriers
+
+struct HeadArgs {
+    const float *xs, *ws;
+    int64_t ld_xs, ld_ws;
+    void *logits;
+    int64_t ld;
+    uint32_t B, V, kblocks;
+    uint32_t m_tiles;
+    int64_t tiles;
+    uint32_t x_bytes;          // of one stage's block of hidden states
+    uint32_t stages;
+    const int32_t *ctx;
+    int W;
+    uint32_t vocab_offset;
+    BiasParams bias;
+};
+
+// ---- one-line PTX ---------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+// Waits for the phase of the given parity to end; false if it did not within the limit or, where
+// `gave_up` is given, another thread of the CTA gave up.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up) {
+    if (barrier_try(bar, parity)) return true;
+    const uint64_t start = now_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i)
+            if (barrier_try(bar, parity)) return true;
+        if (gave_up && *gave_up) return false;
+        if (now_ns() - start > kWaitLimit) {
+            if (gave_up) *gave_up = 1u;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ void copy_block(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// Operand block in shared memory: rows of 128 bytes, 128-byte swizzle, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 |
+           uint64_t(2) << 61;
+}
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t form, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(form), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 32 columns of a warp's 32 lanes; the values may be used after read_done on the same array.
+__device__ __forceinline__ void read_columns(uint32_t (&r)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void read_done(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                   "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                   "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// ---- the epilogue's last step ---------------------------------------------------------------
+
+// A row's seed as it is handed from lane to lane.
+template <int SCHEME>
+__device__ __forceinline__ uint64_t row_seed(const HeadArgs &a, int64_t row) {
+    if constexpr (SCHEME == SBW_SCHEME_CONTEXT) return seed_context(a.bias.key, a.ctx + row * a.W, a.W);
+    else if constexpr (SCHEME == SBW_SCHEME_SELFSALT) return jenkins_min(a.ctx + row * a.W, a.W);
+    else return 0;
+}
+template <int SCHEME, int N>
+__device__ __forceinline__ void green_words(uint64_t seed, uint32_t vg, const BiasParams &p, uint32_t (&x)[N]) {
+    RowSeedS<SCHEME> rs;
+    if constexpr (SCHEME == SBW_SCHEME_CONTEXT) rs.rk = make_row_keys(seed);
+    else rs.jmin = static_cast<uint32_t>(seed);
+    rs.template word0_n<N>(vg, p.key, p.weyl, x);
+}
+
+// Writes 32 words (32 fp32 logits, or 64 bf16 ones in pairs) per row of the warp's rows: the words have
+// been laid out in shared memory by row = lane and leave it by column = lane, so that a row is one
+// 128-byte store.
+template <int DTYPE, int SCHEME>
+__device__ __forceinline__ void store_chunk(const HeadArgs &a, const uint32_t *staged, int rows, int64_t row0, uint32_t col0,
+                                            uint64_t seed, int lane) {
+    constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2;
+    const uint32_t col = col0 + lane * PER;
+    char *const base = static_cast<char *>(a.logits) + (row0 * a.ld + col) * (4 / PER);
+    const int64_t stride = a.ld * (4 / PER);
+    const bool whole = col + PER <= a.V && (PER == 1 || (reinterpret_cast<uintptr_t>(base) % 4 == 0 && stride % 4 == 0));
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+        uint32_t w = staged[r * 33 + lane];
+        if constexpr (SCHEME != kSchemeNone) {
+            uint32_t x[PER];
+            green_words<SCHEME, PER>(__shfl_sync(0xffffffffu, seed, r), a.vocab_offset + col, a.bias, x);
+            if constexpr (DTYPE == SBW_DTYPE_F32) {
+                if (x[0] <= a.bias.thr_m1) w = __float_as_uint(__fadd_rn(__uint_as_float(w), a.bias.delta));
+            } else {
+                w = add_bf16x2(w, (x[0] <= a.bias.thr_m1 ? a.bias.delta_bf16 : 0x8000u) |
+                                      (x[1] <= a.bias.thr_m1 ? a.bias.delta_bf16 << 16 : 0x80000000u));
+            }
+        }
+        char *const at = base + r * stride;
+        if (!SBW_CHECKED(col >= a.V || row0 + r < a.B, SBW_SITE_HEAD_STORE)) continue;
+        if (whole) {
+            *reinterpret_cast<uint32_t *>(at) = w;
+        } else if constexpr (PER == 2) {
+            if (col < a.V) *reinterpret_cast<uint16_t *>(at) = static_cast<uint16_t>(w);
+            if (col + 1 < a.V) *reinterpret_cast<uint16_t *>(at + 2) = static_cast<uint16_t>(w >> 16);
+        }
+    }
+}
+
+template <int DTYPE, int SCHEME, int BN>
+__global__ void __launch_bounds__(kHeadThreads, 1)
+    head_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const HeadArgs a) {
+    constexpr int HALF = BN / 2;                       // columns of one warpgroup of the epilogue
+    constexpr int NBUF = kTmemColumns / BN;            // accumulators
+    constexpr uint32_t kWBytes = BN * kBlock;
+    // fp32 accumulator, both operands e4m3 with K along their rows, 128 x BN
+    constexpr uint32_t kForm = 1u << 4 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(kTileM / 16) << 24;
+    extern __shared__ uint8_t dynamic_smem[];
+    __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 2 * NBUF + 1];
+    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t gave_up_slot;
+    volatile uint32_t *const gave_up = &gave_up_slot;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t stages_at = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
+    const uint32_t stage_bytes = kWBytes + a.x_bytes;
+    uint32_t *const staging = reinterpret_cast<uint32_t *>(
+        dynamic_smem + (stages_at - smem_addr(dynamic_smem)) + a.stages * stage_bytes);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
+    const uint32_t ready = empty + 8 * kMaxStages, taken = ready + 8 * NBUF, last = taken + 8 * NBUF;
+
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < kMaxStages; ++i) {
+            barrier_init(full + 8 * i, 1);
+            barrier_init(empty + 8 * i, 1);
+        }
+        for (uint32_t i = 0; i < NBUF; ++i) {
+            barrier_init(ready + 8 * i, 1);
+            barrier_init(taken + 8 * i, kEpilogueWarps);
+        }
+        barrier_init(last, 1);
+        gave_up_slot = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)),
+                     "r"(kTmemColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (warp < 4) {
+        if (warp == 0 && lane == 0) {
+            uint32_t stage = 0, parity = 0;
+            int64_t issued = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+                const int m0 = static_cast<int>(t % a.m_tiles) * kTileM, v0 = static_cast<int>(t / a.m_tiles) * BN;
+                for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
+                    ok = barrier_wait(empty + 8 * stage, parity ^ 1u, gave_up);
+                    if (!ok) break;
+                    const uint32_t at = stages_at + stage * stage_bytes;
+                    barrier_expect(full + 8 * stage, stage_bytes);
+                    copy_block(at, &map_w, static_cast<int>(kb) * kBlock, v0, full + 8 * stage);
+                    copy_block(at + kWBytes, &map_x, static_cast<int>(kb) * kBlock, m0, full + 8 * stage);
+                    ++issued;
+                    if (++stage == a.stages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                }
+            }
+            if (!ok) {       // copies in flight have to land before the CTA's shared memory goes
+                for (uint32_t i = 0; i < a.stages && issued > 0; ++i) {
+                    --issued;
+                    barrier_wait(full + 8 * static_cast<uint32_t>(issued % a.stages),
+                                 static_cast<uint32_t>(issued / a.stages) & 1u, nullptr);
+                }
+            }
+        } else if (warp == 1 && lane == 0) {
+            uint32_t stage = 0, parity = 0, buf = 0, buf_parity = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+                for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
+                    ok = barrier_wait(taken + 8 * buf, buf_parity ^ 1u, gave_up) &&
+                         barrier_wait(full + 8 * stage, parity, gave_up);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = stages_at + stage * stage_bytes;
+                    const uint64_t x = operand(at + kWBytes), w = operand(at);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)        // 32 of a block's 128 at a time: 32 bytes further on in every row
+                        multiply(tmem + buf * BN, x + 2 * k, w + 2 * k, kForm, k > 0);
+                    commit(empty + 8 * stage);
+                    commit(ready + 8 * buf);
+                    if (++stage == a.stages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                    if (++buf == NBUF) {
+                        buf = 0;
+                        buf_parity ^= 1u;
+                    }
+                }
+            }
+            commit(last);                              // no product is in flight when the tensor memory goes
+            barrier_wait(last, 0u, nullptr);
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp % 4, half = (warp - 4) / 4;
+        uint32_t *const staged = staging + (warp - 4) * kStageWords;
+        uint32_t buf = 0, parity = 0;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
+            const int64_t row0 = (t % a.m_tiles) * kTileM + quarter * 32;
+            const uint32_t col0 = static_cast<uint32_t>(t / a.m_tiles) * BN + half * HALF;
+            const int64_t left = static_cast<int64_t>(a.B) - row0;
+            const int rows = left < 0 ? 0 : left < 32 ? static_cast<int>(left) : 32;
+            const int64_t row = row0 + (lane < rows ? lane : 0);
+            const uint32_t vb = min(col0, a.V - 1) / kBlock;
+            const float *const ws = a.ws + static_cast<int64_t>(vb) * a.ld_ws;
+            const float *const xs = a.xs + (rows ? row : 0) * a.ld_xs;
+            float acc[HALF];
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) acc[i] = 0.0f;
+            float next = __ldg(xs) * __ldg(ws);
+            for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
+                const float s = next;
+                if (kb + 1 < a.kblocks) next = __ldg(xs + kb + 1) * __ldg(ws + kb + 1);
+                if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (rows) {
+                    const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + half * HALF;
+                    uint32_t r[2][32];
+                    read_columns(r[0], from);
+#pragma unroll
+                    for (int c = 0; c < HALF / 32; ++c) {
+                        read_done(r[c & 1]);
+                        if (c + 1 < HALF / 32) read_columns(r[(c + 1) & 1], from + 32 * (c + 1));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            acc[32 * c + i] = __fmaf_rn(__uint_as_float(r[c & 1][i]), s, acc[32 * c + i]);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(taken + 8 * buf);
+                if (++buf == NBUF) {
+                    buf = 0;
+                    parity ^= 1u;
+                }
+            }
+            if (!rows) continue;
+            if (!ok) {
+#pragma unroll
+                for (int i = 0; i < HALF; ++i) acc[i] = __uint_as_float(0x7fffffffu);
+            }
+            uint64_t seed = 0;
+            if constexpr (SCHEME != kSchemeNone) seed = row_seed<SCHEME>(a, row);
+            constexpr int CHUNK = DTYPE == SBW_DTYPE_F32 ? 32 : 64;
+#pragma unroll
+            for (int c = 0; c < HALF / CHUNK; ++c) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    if constexpr (DTYPE == SBW_DTYPE_F32) {
+                        staged[lane * 33 + i] = __float_as_uint(acc[CHUNK * c + i]);
+                    } else {
+                        const __nv_bfloat162 p = __floats2bfloat162_rn(acc[CHUNK * c + 2 * i], acc[CHUNK * c + 2 * i + 1]);
+                        staged[lane * 33 + i] = *reinterpret_cast<const uint32_t *>(&p);
+                    }
+                }
+                __syncwarp();
+                if (col0 + CHUNK * c < a.V) store_chunk<DTYPE, SCHEME>(a, staged, rows, row0, col0 + CHUNK * c, seed, lane);
+                __syncwarp();
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
+    }
+}
+
+// ---- host -----------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode_entry(EncodeTiled *out) {
+    static std::atomic<void *> found{nullptr};
+    void *p = found.load(std::memory_order_acquire);
+    if (!p) {
+        cudaDriverEntryPointQueryResult status;
+        SBW_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &status));
+        if (status != cudaDriverEntryPointSuccess || !p) return SBW_ERR_UNSUPPORTED;
+        found.store(p, std::memory_order_release);
+    }
+    *out = reinterpret_cast<EncodeTiled>(p);
+    return SBW_OK;
+}
+
+// A [rows, K] operand copied in blocks of box_rows rows by 128 bytes; what lies outside reads as 0.
+int make_map(CUtensorMap *map, const void *p, int64_t rows, int64_t K, int64_t ld, int box_rows) {
+    EncodeTiled encode;
+    if (int rc = encode_entry(&encode)) return rc;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
+    const cuuint32_t box[2] = {kBlock, static_cast<cuuint32_t>(box_rows)}, unit[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), dims, strides, box, unit,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue);
+    return SBW_OK;
+}
+
+template <int DTYPE, int SCHEME, int BN>
+int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t ld_w, int64_t K, cudaStream_t stream) {
+    DeviceInfo di;
+    if (int rc = current_device_info(&di)) return rc;
+    const int box_m = a.B < kTileM ? static_cast<int>((a.B + 7) / 8 * 8) : kTileM;
+    a.x_bytes = static_cast<uint32_t>(box_m) * kBlock;
+    const uint32_t stage_bytes = BN * kBlock + a.x_bytes;
+    // the matrix unit reads 128 rows of hidden states whatever x_bytes is: behind the last stage lies the
+    // staging area, which is larger than what that takes
+    static_assert(kStagingBytes >= kTileM * kBlock, "");
+    a.stages = (kMaxDynamicBytes - 1024 - kStagingBytes) / stage_bytes;
+    if (a.stages > kMaxStages) a.stages = kMaxStages;
+    const size_t bytes = 1024 + a.stages * stage_bytes + kStagingBytes;
+    a.m_tiles = (a.B + kTileM - 1) / kTileM;
+    a.tiles = static_cast<int64_t>(a.m_tiles) * ((a.V + BN - 1) / BN);
+    CUtensorMap map_x, map_w;
+    if (int rc = make_map(&map_x, x, a.B, K, ld_x, box_m)) return rc;
+    if (int rc = make_map(&map_w, w, a.V, K, ld_w, BN)) return rc;
+    const auto kernel = head_kernel<DTYPE, SCHEME, BN>;
+    static std::atomic<uint64_t> prepared{0};
+    if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
+        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynamicBytes));
+        prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.tiles < di.sm_count ? a.tiles : di.sm_count));
+    cfg.blockDim = dim3(kHeadThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, map_x, map_w, a));
+    return SBW_OK;
+}
+
+template <int DTYPE, int SCHEME>
+int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t ld_w, int64_t K, cudaStream_t s) {
+    // up to 128 rows the weights' bytes bound the call and narrower tiles share them out more evenly;
+    // above, each byte of a wider tile's weights serves more products
+    return a.B <= kTileM ? launch_head<DTYPE, SCHEME, 128>(a, x, ld_x, w, ld_w, K, s)
+                         : launch_head<DTYPE, SCHEME, 256>(a, x, ld_x, w, ld_w, K, s);
+}
+
+}  // namespace
+}  // namespace sbw
+
+extern "C" int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scales, int64_t ld_x_scales, const void *w,
+                               int64_t ld_w, const float *w_scales, int64_t ld_w_scales, int64_t B, int64_t V, int64_t K,
+                               void *logits, int dtype, int64_t ld, int64_t vocab_offset, const int32_t *ctx_tokens,
+                               int ctx_width, uint64_t key, double gamma, float delta, int scheme, void *stream) {
+    using namespace sbw;
+    if (!valid_common(dtype, ctx_width, gamma, scheme)) return SBW_ERR_INVALID_ARG;
+    if (B < 0 || V <= 0 || K <= 0 || ld < V || vocab_offset < 0) return SBW_ERR_INVALID_ARG;
+    if (!(delta == delta) || delta - delta != 0.0f) return SBW_ERR_INVALID_ARG;
+    constexpr int64_t kMost = 0x7fffffffLL - 256;           // coordinates of the copies are 32-bit
+    if (B > kMost || V > kMost || K > kMost || vocab_offset + V > (int64_t(1) << 32)) return SBW_ERR_UNSUPPORTED;
+    const int64_t kblocks = (K + kBlock - 1) / kBlock;
+    if (ld_x < K || ld_w < K || ld_x_scales < kblocks || ld_w_scales < kblocks) return SBW_ERR_INVALID_ARG;
+    if (B == 0) return SBW_OK;
+    const float in_precision = dtype == SBW_DTYPE_BF16 ? __bfloat162float(__float2bfloat16_rn(delta)) : delta;
+    const bool marked = in_precision != 0.0f;
+    if (!x || !x_scales || !w || !w_scales || !logits || (marked && !ctx_tokens)) return SBW_ERR_INVALID_ARG;
+    // operands are copied by tensor maps: 16-byte aligned rows
+    if (reinterpret_cast<uintptr_t>(x) % 16 != 0 || reinterpret_cast<uintptr_t>(w) % 16 != 0) return SBW_ERR_INVALID_ARG;
+    if ((B > 1 && ld_x % 16 != 0) || (V > 1 && ld_w % 16 != 0)) return SBW_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(x_scales) % 4 != 0 || reinterpret_cast<uintptr_t>(w_scales) % 4 != 0 ||
+        reinterpret_cast<uintptr_t>(logits) % (dtype == SBW_DTYPE_F32 ? 4 : 2) != 0)
+        return SBW_ERR_INVALID_ARG;
+    if (B == 1) ld_x = (K + 15) / 16 * 16;
+    if (V == 1) ld_w = (K + 15) / 16 * 16;
+    if (ld_x >= (int64_t(1) << 40) || ld_w >= (int64_t(1) << 40)) return SBW_ERR_UNSUPPORTED;
+    HeadArgs a = {};
+    a.xs = x_scales;
+    a.ws = w_scales;
+    a.ld_xs = ld_x_scales;
+    a.ld_ws = ld_w_scales;
+    a.logits = logits;
+    a.ld = ld;
+    a.B = static_cast<uint32_t>(B);
+    a.V = static_cast<uint32_t>(V);
+    a.kblocks = static_cast<uint32_t>(kblocks);
+    a.ctx = ctx_tokens;
+    a.W = ctx_width;
+    a.vocab_offset = static_cast<uint32_t>(vocab_offset);
+    a.bias.key = key;
+    a.bias.thr_m1 = threshold_minus_one(gamma);
+    a.bias.delta = in_precision;
+    a.bias.delta_bf16 = dtype == SBW_DTYPE_BF16 ? static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(delta))) : 0u;
+    a.bias.weyl = make_weyl();
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype == SBW_DTYPE_F32) {
+        if (!marked) return launch_head<SBW_DTYPE_F32, kSchemeNone>(a, x, ld_x, w, ld_w, K, s);
+        return scheme == SBW_SCHEME_CONTEXT ? launch_head<SBW_DTYPE_F32, SBW_SCHEME_CONTEXT>(a, x, ld_x, w, ld_w, K, s)
+                                            : launch_head<SBW_DTYPE_F32, SBW_SCHEME_SELFSALT>(a, x, ld_x, w, ld_w, K, s);
+    }
+    if (!marked) return launch_head<SBW_DTYPE_BF16, kSchemeNone>(a, x, ld_x, w, ld_w, K, s);
+    return scheme == SBW_SCHEME_CONTEXT ? launch_head<SBW_DTYPE_BF16, SBW_SCHEME_CONTEXT>(a, x, ld_x, w, ld_w, K, s)
+                                        : launch_head<SBW_DTYPE_BF16, SBW_SCHEME_SELFSALT>(a, x, ld_x, w, ld_w, K, s);
+}
