@@ -510,6 +510,42 @@ int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scales, int64_t 
                     void *logits, int dtype, int64_t ld, int64_t vocab_offset, const int32_t *ctx_tokens,
                     int ctx_width, uint64_t key, double gamma, float delta, int scheme, void *stream);
 
+/*
+ * sbw_sample_given -- one token per row from a random number that the caller gives, with temperature, top-k, top-p
+ * and min-p of its own for every row (a serving batch in which each request has its settings; random numbers from
+ * the caller's generator, or shared with another sampler).  Per row b, with l' the biased logits of Eq. 2 in the logits' own
+ * precision (the logits themselves where delta is 0 in it):
+ *   order    candidates are ranked by value, descending, equal ones by column (-0 equals +0; NaN counts as -inf);
+ *            m is the first one's value.
+ *   weights  with tau = temperature[b], c = (float)(log2(e) / (double)tau), y = (l' - m) c in fp32: W = 0 if not
+ *            y >= -41, else trunc(2^(40 + n) P(y - n)), n = rintf(y), P as in sbw_bias_sample_filtered (which has the
+ *            same weights).  Sums of weights are exact.  A candidate of weight 0 is never kept.
+ *   min_p    > 0 drops the candidates with y < (float)log2((double)min_p[b]) (values above 1 count as 1: what equals
+ *            m stays).
+ *   top_k    > 0 keeps the first top_k[b] of what is left.
+ *   top_p    < 1 keeps a candidate of what is left then iff the weights before it sum to S with
+ *            S 2^32 < max(1, floor(top_p[b] 2^32)) Z, Z being the sum over all of them.
+ *   draw     with Z the sum over what is kept: the first kept candidate, in the order above, at which the running weight
+ *            exceeds floor(u 2^32) Z / 2^32, u = uniforms[b] (values below 0 and NaN count as 0, values from 1 on as
+ *            the largest number below).  u = 0 is the most probable candidate.
+ * A temperature below 1e-6, or NaN, is greedy: the first candidate of the order.  A NaN among min_p or top_p switches
+ * that filter off for its row, as do min_p <= 0, top_k <= 0 and top_p >= 1.
+ *   logits, dtype, B, V, ld, vocab_offset, ctx_tokens, ctx_width, key, gamma, delta, scheme   as for
+ *               sbw_token_logprobs (read only; rows of any alignment take the vectorised path; a row holds its whole
+ *               vocabulary).  V <= 262144 (SBW_ERR_TOO_LARGE beyond).
+ *   uniforms, temperature   device [B] float.
+ *   top_k       device [B] int32;  top_p, min_p  device [B] float; each may be NULL: off for every row.
+ *   out_tokens  device [B] int32: the column drawn.
+ *   out_prob    device [B] float or NULL: its weight over Z (its probability among what is kept).
+ *   out_kept    device [B] int32 or NULL: the number of candidates kept.
+ * A row without a value above -inf: token 0, probability 0, kept 0.  +inf among the logits: those share the whole weight.
+ * No workspace; calls on different streams may overlap.
+ */
+int sbw_sample_given(const void *logits, int dtype, int64_t B, int64_t V, int64_t ld, int64_t vocab_offset,
+                     const int32_t *ctx_tokens, int ctx_width, uint64_t key, double gamma, float delta, int scheme,
+                     const float *uniforms, const float *temperature, const int32_t *top_k, const float *top_p,
+                     const float *min_p, int32_t *out_tokens, float *out_prob, int32_t *out_kept, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

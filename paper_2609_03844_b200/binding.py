@@ -36,7 +36,7 @@ EXPORTS = ("sbw_version", "sbw_last_cuda_error", "sbw_bias_logits",
            "sbw_roc_auc_workspace_bytes", "sbw_roc_auc", "sbw_sample_filtered_workspace_bytes",
            "sbw_bias_sample_filtered", "sbw_roc_auc_batched", "sbw_bias_sample_shard_ids",
            "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted", "sbw_quantize_fp8",
-           "sbw_head_logits")
+           "sbw_head_logits", "sbw_sample_given")
 
 _lib = None
 
@@ -154,6 +154,9 @@ def lib() -> ctypes.CDLL:
         L.sbw_head_logits.restype = i32
         L.sbw_head_logits.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, i64, vp, i32, u64,
                                       c.c_double, c.c_float, i32, vp]
+        L.sbw_sample_given.restype = i32
+        L.sbw_sample_given.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double, c.c_float, i32, vp, vp, vp, vp,
+                                       vp, vp, vp, vp, vp]
         L.sbw_int_probe.restype = i32
         L.sbw_int_probe.argtypes = [i32, i32, i32, i32, vp, vp, vp]
         atexit.register(_drain_at_exit)
@@ -698,6 +701,30 @@ def sbw_head_logits(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_
     _launch("sbw_head_logits", dev, stream, *given, B, V, K, logits.data_ptr(), _dtype_code(logits), ld, vocab_offset, ctx,
             W, key, gamma, delta, scheme)
     return logits
+
+
+def sbw_sample_given(logits: torch.Tensor, uniforms: torch.Tensor, out_tokens: torch.Tensor, *, temperature: torch.Tensor,
+                     top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None,
+                     min_p: torch.Tensor | None = None, out_prob: torch.Tensor | None = None,
+                     out_kept: torch.Tensor | None = None, ctx_tokens: torch.Tensor | None = None, key: int = 0,
+                     gamma: float = 0.5, delta: float = 0.0, scheme: int = SCHEME_CONTEXT, V: int | None = None,
+                     vocab_offset: int = 0, stream=None) -> torch.Tensor:
+    """One token per row of ``logits`` from the given ``uniforms`` (float32 ``[B]``, in [0, 1)) into ``out_tokens``
+    (int32 ``[B]``), with a ``temperature`` (float32 ``[B]``, 0 for greedy) and, where given, ``top_k`` (int32), ``top_p`` and
+    ``min_p`` (float32) per row; ``out_prob`` is the drawn token's probability among the ``out_kept`` candidates that the
+    filters left.  With ``delta`` the watermarked logits are sampled; ``logits`` itself is not changed.  Returns
+    ``out_tokens``."""
+    B, V, ld = _logits_layout("logits", logits, V)
+    dev, f32, i32 = logits.get_device(), torch.float32, torch.int32
+    if uniforms is None or temperature is None or out_tokens is None:
+        raise TypeError("uniforms, temperature and out_tokens are needed")
+    given = _expect(dev, ("uniforms", uniforms, f32, B), ("temperature", temperature, f32, B), ("top_k", top_k, i32, B),
+                    ("top_p", top_p, f32, B), ("min_p", min_p, f32, B), ("out_tokens", out_tokens, i32, B),
+                    ("out_prob", out_prob, f32, B), ("out_kept", out_kept, i32, B))
+    ctx, W = _watermark(ctx_tokens, B, delta, dev)
+    _launch("sbw_sample_given", dev, stream, logits.data_ptr(), _dtype_code(logits), B, V, ld, vocab_offset, ctx, W, key,
+            gamma, delta, scheme, *given)
+    return out_tokens
 
 
 PROBE_KINDS = {"mulwide": (0, 1), "lop3": (1, 1), "iadd3": (2, 1), "imad": (3, 1), "philox": (4, 4),
