@@ -532,7 +532,7 @@ int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scales, int64_t 
  * that filter off for its row, as do min_p <= 0, top_k <= 0 and top_p >= 1.
  *   logits, dtype, B, V, ld, vocab_offset, ctx_tokens, ctx_width, key, gamma, delta, scheme   as for
  *               sbw_token_logprobs (read only; rows of any alignment take the vectorised path; a row holds its whole
- *               vocabulary).  V <= 262144 (SBW_ERR_TOO_LARGE beyond).
+ *               vocabulary).  V <= 327680 (SBW_ERR_TOO_LARGE beyond).
  *   uniforms, temperature   device [B] float.
  *   top_k       device [B] int32;  top_p, min_p  device [B] float; each may be NULL: off for every row.
  *   out_tokens  device [B] int32: the column drawn.

@@ -11,9 +11,9 @@
 // A row is read from memory once.  A cluster of CTAs keeps its biased logits in shared memory, a slice
 // per CTA, and passes over them there:
 //   maximum    while loading
-//   histogram  2048 bins of 1/128 of a power of two below the maximum: number of candidates and sum of
-//              their 25-bit mantissas in two limbs (32-bit counters, native adds; all weights of a bin
-//              share their exponent).  What lies below 2^-15.5 of the maximum is summed in registers.
+//   histogram  1024 bins by the weight's exponent and six bits of its mantissa, down to 2^-16 of the
+//              maximum: the number of candidates and the sum of the other 17 bits (32-bit counters, native
+//              adds).  Weights below that are summed in registers.
 //   lists      the first CTA scans the bins, asks the others for the candidates of the first bins up to
 //              the one that is looked for (of that bin alone if those are too many for the list), sorts
 //              them and walks the running sums.  The first list usually answers all questions.
@@ -35,16 +35,25 @@ namespace cg = cooperative_groups;
 
 constexpr int kGivenThreads = 512;
 constexpr int kGivenWarps = kGivenThreads / 32;
-constexpr int kOctaves = 16;               // of the histogram; below lies the tail
-constexpr int kPerOctave = 128;
-constexpr int kBins = kOctaves * kPerOctave;
-constexpr int kTail = kBins;               // number of the bin of everything below
+// A weight as fp32 bits: 2^40 has exponent 167.  Bins are the bits from the 17th up, counted so that the
+// maximum's is the last one; below the first lies the tail.  The polynomial of the weights is monotone at
+// that resolution (all fp32 arguments were tried; at one bit more it is not), so bins keep the order.
+constexpr int kLowBits = 17;
+constexpr int kBins = 1024;
+constexpr uint32_t kFirstBits = (167u << (23 - kLowBits)) - (kBins - 1);
+constexpr int kTail = -1;                  // number of the bin of everything below
 constexpr int kFine = 1024;                // bins of a split
 constexpr int kListCap = 2048;
+constexpr int kCountingSort = 128;         // a list up to this length is sorted by counting
+constexpr int kPrefixCap = 1024;           // a list from the first candidate on is made up to this length
 constexpr int kMaxParts = 8;
-constexpr int64_t kMaxGivenV = int64_t(1) << 18;     // the upper limb of a bin holds that many candidates
+constexpr int64_t kMaxGivenV = 320 * 1024;
 constexpr int64_t kSliceBytes = 68 * 1024;           // two CTAs with such a slice fit on an SM
-constexpr uint32_t kLimb = 12;
+// A sum of 17 bits holds 32768 candidates: every other warp of a CTA has its own.  The tail's sums in
+// registers hold 128 weights of 25 bits.
+static_assert(kMaxGivenV / kMaxParts <= 61440 && kSliceBytes / 2 <= 61440, "");
+static_assert(kMaxGivenV / kMaxParts + 16 <= 120 * kGivenThreads && kSliceBytes / 2 <= 120 * kGivenThreads, "");
+constexpr uint32_t kLimb = 12;                       // of a split's two sums
 
 struct GivenArgs {
     const void *logits;
@@ -66,37 +75,44 @@ struct GivenArgs {
 enum { kDone = 0, kGather, kSplit, kCountTies, kPickTie };
 struct Command {
     int op;
-    uint32_t bin_lo, bin_hi;   // kGather, kSplit: candidates of these bins ...
+    int bin_lo, bin_hi;        // kGather, kSplit: candidates of these bins ...
     uint32_t dist_lo, dist_hi; // ... whose distance below the maximum (in codes) lies here; ties: dist_lo alone
     uint32_t shift;            // kSplit: distance - dist_lo, by this many bits to the right, is the bin
     uint32_t part, which;      // kPickTie
 };
 
+struct Sums {
+    unsigned long long weight;
+    uint32_t n;
+};
+struct ScanSlots {
+    unsigned long long weight[kGivenWarps];
+    uint32_t n[kGivenWarps];
+};
 struct GivenShared {
-    union {
-        struct {
-            uint32_t n[kBins], lo[kBins], hi[kBins];
-        } hist;                                       // a CTA's own candidates
-        struct {
-            unsigned long long weight[kBins];
-            uint32_t n[kBins];
-        } bins;                                       // first CTA: the row's
-    };
+    struct {
+        uint32_t n[kBins], low[2][kBins];
+    } hist;                                           // a CTA's own candidates
+    struct {
+        unsigned long long weight[kBins];
+        uint32_t n[kBins];
+    } bins;                                           // first CTA: the row's
     union {
         unsigned long long list[kListCap];
         struct {
             uint32_t n[kFine], lo[kFine], hi[kFine];
         } fine;
     };
-    unsigned long long scan[kGivenWarps], scan2[kGivenWarps];
+    ScanSlots scan;
     unsigned long long found_before, found_weight;    // running weight before, own weight
     unsigned long long tail_weight[kMaxParts];
     uint32_t tail_n[kMaxParts];
     float part_max[kMaxParts];
     uint32_t ties[kMaxParts];
     uint32_t tie_col;
-    uint32_t list_n;
-    uint32_t found_at, found_n_before, found_n;
+    uint32_t list_n, list_at;
+    int found_at;
+    uint32_t found_n_before, found_n;
     uint32_t found_dist, found_col;
     float warp_max[kGivenWarps];
     Command cmd;
@@ -104,61 +120,109 @@ struct GivenShared {
 
 // What a row's weights depend on.
 struct RowWeights {
-    float m, c, lowest;        // maximum; log2(e) / temperature; least log2 of a weight over the maximum's
+    float m, c, lowest;        // maximum; log2(e) / temperature; least log2 of a kept weight over the maximum's
     uint32_t code_m;
     __device__ __forceinline__ float log2_of(float x) const { return __fmul_rn(__fsub_rn(x, m), c); }
 };
 
-// 2^y for lowest <= y <= 0 as mantissa 2^24 .. 2^25 (2^f, |f| <= 1/2, in units of 2^-24) and exponent.
-// The polynomial's coefficients are those of the weights of sbw_bias_sample_filtered times 2^24: a power
-// of two changes no rounding.
-__device__ __forceinline__ void power(float y, uint32_t &mantissa, int &n, float &f) {
-    const float t = __fadd_rn(y, 12582912.0f);       // 1.5 2^23: the sum's last bits are rint(y)
-    n = static_cast<int>(__float_as_uint(t) - 0x4b400000u);
-    f = __fsub_rn(y, __fsub_rn(t, 12582912.0f));
-    float p = 0x1.ffcbfcp+7f;
-    p = __fmaf_rn(p, f, 0x1.430912p+11f);
-    p = __fmaf_rn(p, f, 0x1.5d87fep+14f);
-    p = __fmaf_rn(p, f, 0x1.3b2ab6p+17f);
-    p = __fmaf_rn(p, f, 0x1.c6b08ep+19f);
-    p = __fmaf_rn(p, f, 0x1.ebfbep+21f);
-    p = __fmaf_rn(p, f, 0x1.62e43p+23f);
-    p = __fmaf_rn(p, f, 0x1p+24f);
-    mantissa = __float2uint_rz(p);
+// Two fp32 operations per instruction.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
 }
-// trunc(2^(40 + y)) from the two: 24 of the 40 bits are in the mantissa.
-__device__ __forceinline__ unsigned long long weight_of(uint32_t mantissa, int n) {
-    return n >= -16 ? static_cast<unsigned long long>(mantissa) << (n + 16) : static_cast<unsigned long long>(mantissa >> (-n - 16));
+__device__ __forceinline__ void of_pair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
-__device__ __forceinline__ uint32_t bin_of(int n, float f) {
-    const int sub = __float2int_rz(__fmaf_rn(f, -static_cast<float>(kPerOctave), 0.5f * kPerOctave));
-    return static_cast<uint32_t>(-n * kPerOctave + (sub < kPerOctave ? sub : kPerOctave - 1));
+__device__ __forceinline__ Pair pair_mul(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
 }
 
-__device__ __forceinline__ unsigned long long warp_inclusive(unsigned long long x, int lane) {
+// 2^(40 + y) as fp32 for two y in [-41, 0]; anything for others.  The steps and coefficients are those of the
+// weights of sbw_bias_sample_filtered, the latter times 2^40: a power of two changes no rounding.  The weight is what
+// truncation leaves of it.
+constexpr float kRound = 12582912.0f;                // 1.5 2^23: the last bits of y + kRound are rint(y)
+__device__ __forceinline__ void power(Pair y, uint32_t &v0, uint32_t &v1) {
+    const Pair t = pair_add(y, pair_of(kRound, kRound));
+    const Pair f = pair_fma(pair_add(t, pair_of(-kRound, -kRound)), pair_of(-1.0f, -1.0f), y);
+    Pair p = pair_of(0x1.ffcbfcp+23f, 0x1.ffcbfcp+23f);
+    p = pair_fma(p, f, pair_of(0x1.430912p+27f, 0x1.430912p+27f));
+    p = pair_fma(p, f, pair_of(0x1.5d87fep+30f, 0x1.5d87fep+30f));
+    p = pair_fma(p, f, pair_of(0x1.3b2ab6p+33f, 0x1.3b2ab6p+33f));
+    p = pair_fma(p, f, pair_of(0x1.c6b08ep+35f, 0x1.c6b08ep+35f));
+    p = pair_fma(p, f, pair_of(0x1.ebfbep+37f, 0x1.ebfbep+37f));
+    p = pair_fma(p, f, pair_of(0x1.62e43p+39f, 0x1.62e43p+39f));
+    p = pair_fma(p, f, pair_of(0x1p+40f, 0x1p+40f));
+    float p0, p1, t0, t1;
+    of_pair(p, p0, p1);
+    of_pair(t, t0, t1);
+    v0 = __float_as_uint(p0) + (__float_as_uint(t0) << 23);      // the low bits of kRound are 0: n goes to the exponent
+    v1 = __float_as_uint(p1) + (__float_as_uint(t1) << 23);
+}
+__device__ __forceinline__ uint32_t power(float y) {
+    uint32_t v, other;
+    power(pair_of(y, y), v, other);
+    return v;
+}
+__device__ __forceinline__ int bin_of(uint32_t v) {
+    const int b = static_cast<int>(v >> kLowBits) - static_cast<int>(kFirstBits);
+    return b < 0 ? kTail : b;
+}
+// Bits by which a weight of a bin is shifted to the left of its 24-bit mantissa.
+__device__ __forceinline__ int shift_of_bin(int bin) {
+    return static_cast<int>((static_cast<uint32_t>(bin) + kFirstBits) >> (23 - kLowBits)) - 150;
+}
+__device__ __forceinline__ unsigned long long weight_of(uint32_t v) {
+    const int up = static_cast<int>(v >> 23) - 150;
+    const uint32_t mantissa = (v & 0x7fffffu) | 0x800000u;
+    return up >= 0 ? static_cast<unsigned long long>(mantissa) << up : up > -32 ? static_cast<unsigned long long>(mantissa >> -up) : 0ull;
+}
+
+// Exclusive prefixes of a weight and a number over the CTA in thread order, and the totals.
+__device__ __forceinline__ Sums block_before(unsigned long long weight, uint32_t n, ScanSlots &slots, Sums &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long w = weight;
+    uint32_t m = n;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long up = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += up;
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, w, d);
+        const uint32_t up_n = __shfl_up_sync(0xffffffffu, m, d);
+        if (lane >= d) {
+            w += up;
+            m += up_n;
+        }
     }
-    return x;
-}
-// Exclusive prefix over the CTA in thread order, and the total.
-__device__ __forceinline__ unsigned long long block_before(unsigned long long x, unsigned long long *slots, unsigned long long &total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const unsigned long long incl = warp_inclusive(x, lane);
     __syncthreads();
-    if (lane == 31) slots[warp] = incl;
+    if (lane == 31) {
+        slots.weight[warp] = w;
+        slots.n[warp] = m;
+    }
     __syncthreads();
-    unsigned long long before = 0;
-    total = 0;
+    Sums before = {w - weight, m - n};
+    total = {0, 0};
 #pragma unroll
-    for (int w = 0; w < kGivenWarps; ++w) {
-        const unsigned long long s = slots[w];
-        if (w < warp) before += s;
-        total += s;
+    for (int i = 0; i < kGivenWarps; ++i) {
+        const unsigned long long x = slots.weight[i];
+        const uint32_t y = slots.n[i];
+        if (i < warp) {
+            before.weight += x;
+            before.n += y;
+        }
+        total.weight += x;
+        total.n += y;
     }
-    return before + incl - x;
+    return before;
 }
 
 // floor(a b / 2^32) and whether something is left over, for a product of up to 96 bits.
@@ -179,15 +243,8 @@ struct Row {
         if constexpr (DTYPE == SBW_DTYPE_F32) return __uint_as_float(e[i]);
         else return __uint_as_float((i & 1) ? (e[i >> 1] & 0xffff0000u) : (e[i >> 1] << 16));
     }
-    // f(value, column) for every element
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) {
-            const uint4 w = slice[j];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) f(value(w, i), col0 + j * VEC + i);
-        }
-    }
+    // Element i of the thread's vector w, and the next, as a pair.
+    static __device__ __forceinline__ Pair values(const uint4 &w, int i) { return pair_of(value(w, i), value(w, i + 1)); }
 };
 
 // -0 becomes +0 and NaN becomes -inf, in every element.
@@ -253,6 +310,13 @@ __device__ __forceinline__ float load_slice(const GivenArgs &a, int64_t row, uin
     return best;
 }
 
+// One add to shared memory under a condition, as a predicated instruction: a branch per element would keep the
+// elements of a vector from overlapping.
+__device__ __forceinline__ void add_if(bool yes, uint32_t addr, uint32_t x) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.relaxed.cta.shared::cta.add.u32 [%0], %1;\n\t}"
+                 ::"r"(addr), "r"(x), "r"(static_cast<uint32_t>(yes)) : "memory");
+}
+
 template <int DTYPE>
 class Cluster {
   public:
@@ -274,117 +338,133 @@ class Cluster {
     }
     __device__ __forceinline__ uint32_t distance(float x) const { return rw.code_m - order_code(__float_as_uint(x)); }
     __device__ __forceinline__ unsigned long long weight_at(uint32_t dist) const {
-        uint32_t mantissa;
-        int n;
-        float f;
-        power(rw.log2_of(__uint_as_float(order_decode(rw.code_m - dist))), mantissa, n, f);
-        return weight_of(mantissa, n);
+        return weight_of(power(rw.log2_of(__uint_as_float(order_decode(rw.code_m - dist)))));
+    }
+    __device__ __forceinline__ Pair log2_of(Pair x) const {
+        return pair_mul(pair_add(x, pair_of(-rw.m, -rw.m)), pair_of(rw.c, rw.c));
     }
 
-    // The CTA's candidates in bins, those of the tail summed.
+    // The CTA's candidates in bins, those of the tail summed.  No branch, so that the elements of a vector overlap.
     __device__ __forceinline__ void histogram() const {
-        for (int i = threadIdx.x; i < kBins; i += kGivenThreads) sh.hist.n[i] = sh.hist.lo[i] = sh.hist.hi[i] = 0u;
+        for (int i = threadIdx.x; i < kBins; i += kGivenThreads) sh.hist.n[i] = sh.hist.low[0][i] = sh.hist.low[1][i] = 0u;
         __syncthreads();
-        unsigned long long weight = 0;
-        uint32_t number = 0;
-        row.each([&](float x, uint32_t) {
-            const float y = rw.log2_of(x);
-            if (!(y >= rw.lowest)) return;
-            uint32_t mantissa;
-            int n;
-            float f;
-            power(y, mantissa, n, f);
-            if (n > -kOctaves) {
-                const uint32_t bin = bin_of(n, f);
-                atomicAdd(&sh.hist.n[bin], 1u);
-                atomicAdd(&sh.hist.lo[bin], mantissa & ((1u << kLimb) - 1u));
-                atomicAdd(&sh.hist.hi[bin], mantissa >> kLimb);
-            } else {
-                const uint32_t w = mantissa >> (-n - 16);
-                weight += w;
-                number += w != 0u;
+        // addresses less what the first bin's bits come to
+        const uint32_t at_n = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.n)) - 4u * kFirstBits;
+        const uint32_t at_low = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.low[(threadIdx.x >> 5) & 1])) - 4u * kFirstBits;
+        uint32_t tail = 0, number = 0;
+        for (uint32_t j = threadIdx.x; j < row.vectors; j += kGivenThreads) {
+            const uint4 w = row.slice[j];
+#pragma unroll
+            for (int i = 0; i < Row<DTYPE>::VEC; i += 2) {
+                const Pair y = log2_of(Row<DTYPE>::values(w, i));
+                float yy[2];
+                uint32_t v[2];
+                of_pair(y, yy[0], yy[1]);
+                power(y, v[0], v[1]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t u = yy[k] >= rw.lowest ? v[k] : 0u;
+                    const bool binned = u >= kFirstBits << kLowBits;
+                    const uint32_t four_bin = u >> (kLowBits - 2) & ~3u;
+                    add_if(binned, at_n + four_bin, 1u);
+                    add_if(binned, at_low + four_bin, u & ((1u << kLowBits) - 1u));
+                    const uint32_t whole = binned ? 0u : __float2uint_rz(__uint_as_float(u));
+                    tail += whole;
+                    number += whole != 0u;
+                }
             }
-        });
+        }
         // n and weight of the tail to the first CTA
-        unsigned long long total, total_n;
-        block_before(weight, sh.scan, total);
-        block_before(number, sh.scan2, total_n);
+        Sums total;
+        block_before(tail, number, sh.scan, total);
         if (threadIdx.x == 0) {
-            at(sh.tail_weight, 0)[part] = total;
-            at(sh.tail_n, 0)[part] = static_cast<uint32_t>(total_n);
+            at(sh.tail_weight, 0)[part] = total.weight;
+            at(sh.tail_n, 0)[part] = total.n;
         }
     }
 
     // Every CTA adds up a share of the bins over all CTAs and hands it to the first.
     __device__ __forceinline__ void merge() const {
         sync();
-        constexpr int kMost = kBins / kGivenThreads;
         const uint32_t share = kBins / parts;            // a power of two
-        uint32_t n[kMost];
-        unsigned long long w[kMost];
+        for (uint32_t i = threadIdx.x; i < share; i += kGivenThreads) {
+            const uint32_t bin = part * share + i;
+            uint32_t n = 0;
+            unsigned long long low = 0;
 #pragma unroll
-        for (int k = 0; k < kMost; ++k) {
-            const uint32_t in_share = k * kGivenThreads + threadIdx.x, bin = part * share + in_share;
-            n[k] = 0;
-            unsigned long long lo = 0, hi = 0;
-            if (in_share < share) {
-                for (uint32_t r = 0; r < parts; ++r) {
-                    n[k] += at(&sh.hist.n[bin], r)[0];
-                    lo += at(&sh.hist.lo[bin], r)[0];
-                    hi += at(&sh.hist.hi[bin], r)[0];
-                }
+            for (uint32_t r = 0; r < kMaxParts; ++r) {       // unrolled: the loads from other SMs overlap
+                if (r >= parts) break;
+                n += *at(&sh.hist.n[bin], r);
+                low += static_cast<unsigned long long>(*at(&sh.hist.low[0][bin], r)) + *at(&sh.hist.low[1][bin], r);
             }
-            w[k] = (lo + (hi << kLimb)) << (16 - static_cast<int>(bin / kPerOctave));
-        }
-        sync();
-#pragma unroll
-        for (int k = 0; k < kMost; ++k) {
-            const uint32_t in_share = k * kGivenThreads + threadIdx.x, bin = part * share + in_share;
-            if (in_share < share) {
-                at(&sh.bins.n[bin], 0)[0] = n[k];
-                at(&sh.bins.weight[bin], 0)[0] = w[k];
-            }
+            const uint32_t v = (bin + kFirstBits) << kLowBits;       // the bin's least weight
+            *at(&sh.bins.n[bin], 0) = n;
+            *at(&sh.bins.weight[bin], 0) =
+                (static_cast<unsigned long long>(n) * ((v & 0x7fffffu) | 0x800000u) + low) << shift_of_bin(static_cast<int>(bin));
         }
         sync();
     }
 
-    // Whether a candidate belongs to what a command names; its weight's two parts for those that do.
-    __device__ __forceinline__ bool named(const Command &c, float x, uint32_t &mantissa, int &n, uint32_t &dist) const {
-        const float y = rw.log2_of(x);
-        // bins up to bin_hi end above this (half a bin is left for the rounding of the bin's number)
-        const float least = c.bin_hi >= kTail ? rw.lowest : 0.5f - (static_cast<float>(c.bin_hi) + 1.5f) / kPerOctave;
-        if (!(y >= fmaxf(least, rw.lowest))) return false;
-        float f;
-        power(y, mantissa, n, f);
-        const uint32_t bin = n > -kOctaves ? bin_of(n, f) : kTail;
-        if (bin < c.bin_lo || bin > c.bin_hi) return false;
-        if (weight_of(mantissa, n) == 0ull) return false;
-        dist = distance(x);
-        return dist >= c.dist_lo && dist <= c.dist_hi;
+    // f(value, column, weight's bits, distance) for the candidates that a command names.
+    template <typename F>
+    __device__ __forceinline__ void each_named(const Command &c, F f) const {
+        constexpr int VEC = Row<DTYPE>::VEC;
+        // log2 of the bins' ends, with a margin for the rounding of y and of the logarithm
+        const float from = c.bin_lo == kTail ? rw.lowest
+                                             : fmaxf(rw.lowest, __log2f(__uint_as_float((c.bin_lo + kFirstBits) << kLowBits)) - 40.01f);
+        const float to = __log2f(__uint_as_float((c.bin_hi + 1 + kFirstBits) << kLowBits)) - 39.99f;
+        for (uint32_t j = threadIdx.x; j < row.vectors; j += kGivenThreads) {
+            const uint4 w = row.slice[j];
+            uint32_t hits = 0;
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                float y0, y1;
+                of_pair(log2_of(Row<DTYPE>::values(w, i)), y0, y1);
+                if (y0 >= from && y0 <= to) hits |= 1u << i;
+                if (y1 >= from && y1 <= to) hits |= 2u << i;
+            }
+            while (hits) {
+                const int i = __ffs(hits) - 1;
+                hits &= hits - 1u;
+                const float x = Row<DTYPE>::value(row.slice[j], i);
+                const uint32_t v = power(rw.log2_of(x)), dist = distance(x);
+                const int bin = bin_of(v);
+                if (bin >= c.bin_lo && bin <= c.bin_hi && dist >= c.dist_lo && dist <= c.dist_hi) f(row.col0 + j * VEC + i, v, dist);
+            }
+        }
     }
 
     __device__ __forceinline__ void obey(const Command &c) const {
         if (c.op == kGather) {
-            unsigned long long *const list = at(sh.list, 0);
-            uint32_t *const list_n = at(&sh.list_n, 0);
-            row.each([&](float x, uint32_t col) {
-                uint32_t mantissa, dist;
-                int n;
-                if (!named(c, x, mantissa, n, dist)) return;
-                const uint32_t i = atomicAdd(list_n, 1u);
-                if (i < kListCap) list[i] = static_cast<unsigned long long>(dist) << 32 | col;
+            // into the CTA's own list first: an add to another SM's counter takes a microsecond to answer
+            if (part != 0) {
+                if (threadIdx.x == 0) sh.list_n = 0u;
+                __syncthreads();
+            }
+            each_named(c, [&](uint32_t col, uint32_t, uint32_t dist) {
+                const uint32_t i = atomicAdd(&sh.list_n, 1u);
+                if (i < kListCap) sh.list[i] = static_cast<unsigned long long>(dist) << 32 | col;
             });
+            if (part != 0) {
+                __syncthreads();
+                const uint32_t n = min(sh.list_n, static_cast<uint32_t>(kListCap));
+                if (n == 0u) return;
+                if (threadIdx.x == 0) sh.list_at = atomicAdd(at(&sh.list_n, 0), n);
+                __syncthreads();
+                const uint32_t first = sh.list_at;
+                unsigned long long *const list = at(sh.list, 0);
+                for (uint32_t i = threadIdx.x; i < n; i += kGivenThreads)
+                    if (first + i < kListCap) list[first + i] = sh.list[i];
+            }
         } else if (c.op == kSplit) {
             if (part != 0) {                             // the first CTA has cleared its own
                 for (int i = threadIdx.x; i < kFine; i += kGivenThreads) sh.fine.n[i] = sh.fine.lo[i] = sh.fine.hi[i] = 0u;
                 __syncthreads();
             }
-            row.each([&](float x, uint32_t) {
-                uint32_t mantissa, dist;
-                int n;
-                if (!named(c, x, mantissa, n, dist)) return;
+            each_named(c, [&](uint32_t, uint32_t v, uint32_t dist) {
                 const uint32_t bin = (dist - c.dist_lo) >> c.shift;
-                const uint32_t q = n > -kOctaves ? mantissa : mantissa >> (-n - 16);      // of the tail, the weight itself
+                // of a bin the mantissa (the exponent is the bin's), of the tail the weight itself
+                const uint32_t q = c.bin_lo == kTail ? static_cast<uint32_t>(weight_of(v)) : (v & 0x7fffffu) | 0x800000u;
                 atomicAdd(&sh.fine.n[bin], 1u);
                 atomicAdd(&sh.fine.lo[bin], q & ((1u << kLimb) - 1u));
                 atomicAdd(&sh.fine.hi[bin], q >> kLimb);
@@ -410,10 +490,10 @@ class Cluster {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) mine += Row<DTYPE>::value(w, i) == x;
             }
-            unsigned long long total;
-            const uint32_t before = static_cast<uint32_t>(block_before(mine, sh.scan, total));
+            Sums total;
+            const uint32_t before = block_before(0ull, mine, sh.scan, total).n;
             if (c.op == kCountTies) {
-                if (threadIdx.x == 0) at(sh.ties, 0)[part] = static_cast<uint32_t>(total);
+                if (threadIdx.x == 0) at(sh.ties, 0)[part] = total.n;
             } else if (c.part == part && before <= c.which && c.which < before + mine) {
                 uint32_t left = c.which - before;
                 for (uint32_t j = begin; j < end; ++j) {
@@ -457,7 +537,7 @@ class Finder {
     static constexpr int kOwn = kBins / kGivenThreads, kOwnFine = kFine / kGivenThreads, kOwnList = kListCap / kGivenThreads;
     const Cluster<DTYPE> &cl;
     GivenShared &sh;
-    uint32_t own_n0;                       // before this thread's bins
+    uint32_t own_n0;                       // before this thread's bins (which run from the last down)
     unsigned long long own_w0;
     uint32_t bins_n;                       // of all bins but the tail
     unsigned long long bins_w;
@@ -471,15 +551,19 @@ class Finder {
     unsigned long long total_w;
 
     __device__ __forceinline__ explicit Finder(const Cluster<DTYPE> &c) : cl(c), sh(c.sh) {
-        unsigned long long w = 0, n = 0, all;
+        unsigned long long w = 0;
+        uint32_t n = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            w += sh.bins.weight[threadIdx.x * kOwn + i];
-            n += sh.bins.n[threadIdx.x * kOwn + i];
+            w += sh.bins.weight[kBins - 1 - (threadIdx.x * kOwn + i)];
+            n += sh.bins.n[kBins - 1 - (threadIdx.x * kOwn + i)];
         }
-        own_w0 = block_before(w, sh.scan, bins_w);
-        own_n0 = static_cast<uint32_t>(block_before(n, sh.scan2, all));
-        bins_n = static_cast<uint32_t>(all);
+        Sums all;
+        const Sums before = block_before(w, n, sh.scan, all);
+        own_w0 = before.weight;
+        own_n0 = before.n;
+        bins_w = all.weight;
+        bins_n = all.n;
         total_n = bins_n;
         total_w = bins_w;
         for (uint32_t r = 0; r < cl.parts; ++r) {
@@ -500,7 +584,7 @@ class Finder {
     }
 
   private:
-    __device__ __forceinline__ void found_bin(uint32_t at, uint32_t n_before, uint32_t n, unsigned long long w_before, unsigned long long w) {
+    __device__ __forceinline__ void found_bin(int at, uint32_t n_before, uint32_t n, unsigned long long w_before, unsigned long long w) {
         sh.found_at = at;
         sh.found_n_before = n_before;
         sh.found_n = n;
@@ -518,7 +602,8 @@ class Finder {
             unsigned long long w = own_w0;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
-                const uint32_t bin = threadIdx.x * kOwn + i, bn = sh.bins.n[bin];
+                const int bin = kBins - 1 - static_cast<int>(threadIdx.x * kOwn + i);
+                const uint32_t bn = sh.bins.n[bin];
                 const unsigned long long bw = sh.bins.weight[bin];
                 if (by_weight ? w < target && w + bw >= target : n < target && n + bn >= target) found_bin(bin, n, bn, w, bw);
                 n += bn;
@@ -534,8 +619,8 @@ class Finder {
         list_n0 = sh.found_n_before;
         list_w0 = sh.found_before;
         uint32_t number = sh.found_n;
-        if (list_n0 + number <= kListCap) {              // everything from the first candidate on
-            c.bin_lo = 0u;
+        if (list_n0 + number <= kPrefixCap) {            // everything from the first candidate on
+            c.bin_hi = kBins - 1;
             number += list_n0;
             list_n0 = 0u;
             list_w0 = 0ull;
@@ -555,10 +640,9 @@ class Finder {
             c.op = kSplit;
             c.shift = shift;
             cl.order(c);
-            const int octave = static_cast<int>(c.bin_lo / kPerOctave);        // weights of the tail are held as they are
-            const int up = c.bin_lo == kTail ? 0 : 16 - octave;
-            unsigned long long w[kOwnFine], sum_w = 0, sum_n = 0, all;
-            uint32_t n[kOwnFine];
+            const int up = c.bin_lo == kTail ? 0 : shift_of_bin(c.bin_lo);      // weights of the tail are held as they are
+            unsigned long long w[kOwnFine], sum_w = 0;
+            uint32_t n[kOwnFine], sum_n = 0;
 #pragma unroll
             for (int i = 0; i < kOwnFine; ++i) {
                 const int bin = threadIdx.x * kOwnFine + i;
@@ -567,17 +651,19 @@ class Finder {
                 sum_n += n[i];
                 sum_w += w[i];
             }
-            unsigned long long wb = list_w0 + block_before(sum_w, sh.scan, all);
-            uint32_t nb = list_n0 + static_cast<uint32_t>(block_before(sum_n, sh.scan2, all));
+            Sums all;
+            const Sums before = block_before(sum_w, sum_n, sh.scan, all);
+            unsigned long long wb = list_w0 + before.weight;
+            uint32_t nb = list_n0 + before.n;
 #pragma unroll
             for (int i = 0; i < kOwnFine; ++i) {
                 if (by_weight ? wb < target && wb + w[i] >= target : nb < target && nb + n[i] >= target)
-                    found_bin(threadIdx.x * kOwnFine + i, nb, n[i], wb, w[i]);
+                    found_bin(static_cast<int>(threadIdx.x) * kOwnFine + i, nb, n[i], wb, w[i]);
                 nb += n[i];
                 wb += w[i];
             }
             __syncthreads();
-            c.dist_lo += sh.found_at << shift;
+            c.dist_lo += static_cast<uint32_t>(sh.found_at) << shift;
             c.dist_hi = c.dist_lo + ((1u << shift) - 1u);
             list_n0 = sh.found_n_before;
             list_w0 = sh.found_before;
@@ -597,7 +683,9 @@ class Finder {
             item_w[i] = j < list_n ? cl.weight_at(static_cast<uint32_t>(sh.list[j] >> 32)) : 0ull;
             sum += item_w[i];
         }
-        items_w0 = block_before(sum, sh.scan, list_w);
+        Sums all;
+        items_w0 = block_before(sum, 0u, sh.scan, all).weight;
+        list_w = all.weight;
         return false;
     }
 
@@ -624,7 +712,20 @@ class Finder {
         return r;
     }
 
+    // Ascending: a short list by counting the smaller ones, else bitonic.
     __device__ __forceinline__ void sort() {
+        if (list_n <= kCountingSort) {
+            const unsigned long long mine = threadIdx.x < list_n ? sh.list[threadIdx.x] : 0ull;
+            uint32_t rank = 0;
+            if (threadIdx.x < list_n) {
+#pragma unroll 8
+                for (uint32_t i = 0; i < list_n; ++i) rank += sh.list[i] < mine;
+            }
+            __syncthreads();
+            if (threadIdx.x < list_n) sh.list[rank] = mine;
+            __syncthreads();
+            return;
+        }
         uint32_t len = 2;
         while (len < list_n) len <<= 1;
         for (uint32_t i = list_n + threadIdx.x; i < len; i += kGivenThreads) sh.list[i] = ~0ull;
@@ -651,14 +752,14 @@ class Finder {
         for (int i = 0; i < kOwnList; ++i) {
             const uint32_t j = threadIdx.x * kOwnList + i;
             if (j < list_n && (by_weight ? w < target && w + item_w[i] >= target : list_n0 + j + 1u == target)) {
-                found_bin(j, 0u, 0u, w, item_w[i]);
+                found_bin(static_cast<int>(j), 0u, 0u, w, item_w[i]);
                 sh.found_dist = static_cast<uint32_t>(sh.list[j] >> 32);
                 sh.found_col = static_cast<uint32_t>(sh.list[j]);
             }
             w += item_w[i];
         }
         __syncthreads();
-        return Found{sh.found_dist, sh.found_col, list_n0 + sh.found_at + 1u, sh.found_before + sh.found_weight, sh.found_weight};
+        return Found{sh.found_dist, sh.found_col, list_n0 + static_cast<uint32_t>(sh.found_at) + 1u, sh.found_before + sh.found_weight, sh.found_weight};
     }
 };
 
@@ -729,9 +830,9 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
     rw.m = m;
     rw.code_m = order_code(__float_as_uint(m));
     rw.c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
-    rw.lowest = -41.0f;
+    rw.lowest = -40.0f;                                  // below that a weight is 0
     if (!greedy && a.min_p && a.min_p[row] > 0.0f)
-        rw.lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -41.0f), 0.0f);
+        rw.lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -40.0f), 0.0f);
 
     Row<DTYPE> r;
     r.slice = slice;

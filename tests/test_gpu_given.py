@@ -48,7 +48,7 @@ def settings(B, seed):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("B,V,std", [(1, 1, 1.0), (3, 2, 1.0), (5, 7, 3.0), (40, 33, 1.0), (33, 1000, 1.0), (9, 4099, 3.0),
                                      (40, 32003, 3.0), (7, 32000, 1.0), (1, 128256, 4.0), (6, 151936, 1.0), (5, 151937, 4.0),
-                                     (2, 262144, 3.0), (150, 5000, 4.0)])
+                                     (2, 262144, 3.0), (2, 327680, 1.0), (150, 5000, 4.0)])
 def test_rows_with_settings_of_their_own(B, V, std, dtype):
     require_gpu()
     x = inputs.logits_normal(B, V, std, dtype, seed=V + B).cuda()
