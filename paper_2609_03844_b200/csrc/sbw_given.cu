@@ -89,9 +89,10 @@ struct ScanSlots {
     unsigned long long weight[kGivenWarps];
     uint32_t n[kGivenWarps];
 };
+template <int COPIES>
 struct GivenShared {
     struct {
-        uint32_t n[kBins], low[2][kBins];
+        uint32_t n[kBins], low[COPIES][kBins];
     } hist;                                           // a CTA's own candidates
     struct {
         unsigned long long weight[kBins];
@@ -232,21 +233,6 @@ __device__ __forceinline__ unsigned long long share_of(unsigned long long a, uns
     return (hi << 32) | (lo >> 32);
 }
 
-template <int DTYPE>
-struct Row {
-    static constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
-    const uint4 *slice;        // this CTA's vectors
-    uint32_t vectors;
-    uint32_t col0;             // column of its first element; columns before 0 wrap, their values are -inf
-    static __device__ __forceinline__ float value(const uint4 &w, int i) {
-        const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
-        if constexpr (DTYPE == SBW_DTYPE_F32) return __uint_as_float(e[i]);
-        else return __uint_as_float((i & 1) ? (e[i >> 1] & 0xffff0000u) : (e[i >> 1] << 16));
-    }
-    // Element i of the thread's vector w, and the next, as a pair.
-    static __device__ __forceinline__ Pair values(const uint4 &w, int i) { return pair_of(value(w, i), value(w, i + 1)); }
-};
-
 // -0 becomes +0 and NaN becomes -inf, in every element.
 template <int DTYPE>
 __device__ __forceinline__ void settle(uint4 &w) {
@@ -263,53 +249,145 @@ __device__ __forceinline__ void settle(uint4 &w) {
         }
     }
 }
-
-// Loads this CTA's slice of the row, biased, and returns the thread's largest value.
-template <int DTYPE, int SCHEME>
-__device__ __forceinline__ float load_slice(const GivenArgs &a, int64_t row, uint4 *slice, uint32_t vec0, uint32_t vectors, uint32_t head) {
-    constexpr int VEC = Row<DTYPE>::VEC;
-    constexpr int kInFlight = SCHEME == kSchemeNone ? 8 : 2;
-    const char *const row_ptr = static_cast<const char *>(a.logits) + row * a.ld * (16 / VEC);
-    const char *const base = row_ptr - static_cast<int64_t>(head) * (16 / VEC);     // 16-byte aligned
-    RowSeedS<SCHEME> rs;
-    rs.init(a.bias.key, a.ctx + row * a.W, a.W);
-    const uint32_t V = static_cast<uint32_t>(a.V);
-    float best = -INFINITY;
-    for (uint32_t j0 = threadIdx.x; j0 < vectors; j0 += kInFlight * kGivenThreads) {
-        uint4 w[kInFlight];
-        bool whole[kInFlight];
+// The infinite ones share everything: +inf becomes 0 and everything else -inf.
+template <int DTYPE>
+__device__ __forceinline__ void only_infinite(uint4 &w) {
+    uint32_t *e = reinterpret_cast<uint32_t *>(&w);
 #pragma unroll
-        for (int u = 0; u < kInFlight; ++u) {
-            const uint32_t j = j0 + u * kGivenThreads, first = (vec0 + j) * VEC;      // of its elements, head included
-            whole[u] = j < vectors && first >= head && first + VEC <= head + V;
-            w[u] = whole[u] ? __ldcs(reinterpret_cast<const uint4 *>(base) + vec0 + j) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int u = 0; u < kInFlight; ++u) {
-            const uint32_t j = j0 + u * kGivenThreads;
-            if (j >= vectors) break;
-            const uint32_t col = (vec0 + j) * VEC - head;
-            if (whole[u]) {
-                bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col, a.bias);
-            } else {
-                uint32_t *e = reinterpret_cast<uint32_t *>(&w[u]);
-#pragma unroll 1
-                for (int i = 0; i < VEC; ++i) {
-                    float x = -INFINITY;
-                    if (col + i < V) x = biased_at<DTYPE, SCHEME>(row_ptr, col + i, rs, a.vocab_offset + col + i, a.bias);
-                    if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = __float_as_uint(x);
-                    else e[i >> 1] |= (i & 1) ? (__float_as_uint(x) & 0xffff0000u) : (__float_as_uint(x) >> 16);
-                }
-            }
-            settle<DTYPE>(w[u]);
-            slice[j] = w[u];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) best = fmaxf(best, Row<DTYPE>::value(w[u], i));
-        }
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = e[i] == 0x7f800000u ? 0u : 0xff800000u;
+        else e[i] = ((e[i] & 0xffffu) == 0x7f80u ? 0u : 0xff80u) | ((e[i] >> 16) == 0x7f80u ? 0u : 0xff800000u);
     }
-    return best;
 }
 
+// A CTA's part of a row.  Resident: its biased vectors are in shared memory after load().  Otherwise every pass reads
+// them from global memory (the second time from L2) and biases them anew.
+template <int DTYPE_, int SCHEME_, bool RESIDENT_>
+struct Row {
+    static constexpr int DTYPE = DTYPE_, SCHEME = SCHEME_;
+    static constexpr bool RESIDENT = RESIDENT_;
+    static constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
+    using Shared = GivenShared<RESIDENT ? 2 : kGivenWarps>;
+    // loads in flight per thread
+    static constexpr int kInFlight = RESIDENT && SCHEME == kSchemeNone ? 8 : SCHEME == kSchemeNone ? 4 : 2;
+
+    const GivenArgs &a;
+    int64_t row;
+    const char *row_ptr, *base;   // its first element, and the 16-byte boundary at or before it
+    uint32_t head;                // elements between the two
+    uint32_t vec0, vectors;       // this CTA's vectors, counted from base
+    uint32_t col0;                // column of their first element; columns before 0 wrap, their values are -inf
+    uint32_t whole_from, wholes;  // those of the vectors that lie in the row with all their elements
+    uint4 *slice;
+    RowSeedS<SCHEME> rs;
+    bool infinite;
+
+    __device__ __forceinline__ Row(const GivenArgs &args, int64_t r, uint32_t part, uint4 *room)
+        : a(args), row(r), slice(room), infinite(false) {
+        row_ptr = static_cast<const char *>(a.logits) + row * a.ld * (16 / VEC);
+        head = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_ptr) % 16) / (16 / VEC);
+        base = row_ptr - static_cast<int64_t>(head) * (16 / VEC);
+        const uint32_t all = (head + static_cast<uint32_t>(a.V) + VEC - 1) / VEC;
+        vec0 = min(part * a.part_vectors, all);
+        vectors = min(a.part_vectors, all - vec0);
+        col0 = vec0 * VEC - head;
+        whole_from = vec0 == 0u && head ? 1u : 0u;
+        const uint32_t end = (head + static_cast<uint32_t>(a.V)) / VEC;           // of the whole ones, counted from base
+        wholes = min(vec0 + vectors, end) > vec0 + whole_from ? min(vec0 + vectors, end) - (vec0 + whole_from) : 0u;
+        rs.init(a.bias.key, a.ctx + row * a.W, a.W);
+    }
+    __device__ __forceinline__ bool whole(uint32_t j) const { return j - whole_from < wholes; }
+    __device__ __forceinline__ uint4 raw(uint32_t j) const { return __ldg(reinterpret_cast<const uint4 *>(base) + vec0 + j); }
+    // The vector at an end of the row: what lies outside reads as -inf.  Biased.
+    __device__ __forceinline__ uint4 ragged(uint32_t j) const {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        uint32_t *e = reinterpret_cast<uint32_t *>(&w);
+        const uint32_t col = col0 + j * VEC;
+#pragma unroll 1
+        for (int i = 0; i < VEC; ++i) {
+            float x = -INFINITY;
+            if (SBW_CHECKED(j < vectors, SBW_SITE_GIVEN_LOAD) && col + i < static_cast<uint32_t>(a.V))
+                x = biased_at<DTYPE, SCHEME>(row_ptr, col + i, rs, a.vocab_offset + col + i, a.bias);
+            if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = __float_as_uint(x);
+            else e[i >> 1] |= (i & 1) ? (__float_as_uint(x) & 0xffff0000u) : (__float_as_uint(x) >> 16);
+        }
+        return w;
+    }
+    // f(vector, j) for the thread's vectors from global memory, biased
+    template <typename F>
+    __device__ __forceinline__ void each_loaded(F f) const {
+        for (uint32_t j0 = threadIdx.x; j0 < vectors; j0 += kInFlight * kGivenThreads) {
+            uint4 w[kInFlight];
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                const uint32_t j = j0 + u * kGivenThreads;
+                w[u] = whole(j) ? raw(j) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                const uint32_t j = j0 + u * kGivenThreads;
+                if (j >= vectors) break;
+                if (whole(j)) bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col0 + j * VEC, a.bias);
+                else w[u] = ragged(j);
+                f(w[u], j);
+            }
+        }
+    }
+    // f(vector, j) for the thread's vectors, biased and settled
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        if constexpr (RESIDENT) {
+            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(slice[j], j);
+        } else {
+            each_loaded([&](uint4 w, uint32_t j) {
+                settle<DTYPE>(w);
+                if (infinite) only_infinite<DTYPE>(w);
+                f(w, j);
+            });
+        }
+    }
+    // One of them.
+    __device__ __forceinline__ uint4 vector(uint32_t j) const {
+        if constexpr (RESIDENT) return slice[j];
+        uint4 w;
+        if (whole(j)) {
+            w = raw(j);
+            bias_vector<DTYPE, SCHEME>(w, rs, a.vocab_offset + col0 + j * VEC, a.bias);
+        } else {
+            w = ragged(j);
+        }
+        settle<DTYPE>(w);
+        if (infinite) only_infinite<DTYPE>(w);
+        return w;
+    }
+    // Brings a resident part in; returns the thread's largest value.
+    __device__ __forceinline__ float load() {
+        float best = -INFINITY;
+        each_loaded([&](uint4 w, uint32_t j) {
+            settle<DTYPE>(w);
+            if constexpr (RESIDENT) slice[j] = w;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) best = fmaxf(best, value(w, i));
+        });
+        return best;
+    }
+    __device__ __forceinline__ void keep_infinite() {
+        infinite = true;
+        if constexpr (RESIDENT)
+            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) only_infinite<DTYPE>(slice[j]);
+    }
+    static __device__ __forceinline__ float value(const uint4 &w, int i) {
+        const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
+        if constexpr (DTYPE == SBW_DTYPE_F32) return __uint_as_float(e[i]);
+        else return __uint_as_float((i & 1) ? (e[i >> 1] & 0xffff0000u) : (e[i >> 1] << 16));
+    }
+    // Elements i and i + 1 of a vector.
+    static __device__ __forceinline__ Pair values(const uint4 &w, int i) { return pair_of(value(w, i), value(w, i + 1)); }
+};
+
+__device__ __forceinline__ void count_one(uint32_t addr) {
+    asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], %1;" ::"r"(addr), "r"(1u) : "memory");
+}
 // One add to shared memory under a condition, as a predicated instruction: a branch per element would keep the
 // elements of a vector from overlapping.
 __device__ __forceinline__ void add_if(bool yes, uint32_t addr, uint32_t x) {
@@ -317,15 +395,17 @@ __device__ __forceinline__ void add_if(bool yes, uint32_t addr, uint32_t x) {
                  ::"r"(addr), "r"(x), "r"(static_cast<uint32_t>(yes)) : "memory");
 }
 
-template <int DTYPE>
+template <typename ROW>
 class Cluster {
   public:
-    GivenShared &sh;
-    const Row<DTYPE> row;
+    using Shared = typename ROW::Shared;
+    Shared &sh;
+    const ROW &row;
     const RowWeights rw;
     const uint32_t parts, part;
+    static constexpr int kCopies = sizeof(Shared::hist.low) / sizeof(Shared::hist.low[0]);
 
-    __device__ __forceinline__ Cluster(GivenShared &s, const Row<DTYPE> &r, const RowWeights &w, uint32_t n, uint32_t p)
+    __device__ __forceinline__ Cluster(Shared &s, const ROW &r, const RowWeights &w, uint32_t n, uint32_t p)
         : sh(s), row(r), rw(w), parts(n), part(p) {}
 
     __device__ __forceinline__ void sync() const {
@@ -346,17 +426,19 @@ class Cluster {
 
     // The CTA's candidates in bins, those of the tail summed.  No branch, so that the elements of a vector overlap.
     __device__ __forceinline__ void histogram() const {
-        for (int i = threadIdx.x; i < kBins; i += kGivenThreads) sh.hist.n[i] = sh.hist.low[0][i] = sh.hist.low[1][i] = 0u;
+        uint32_t *const all = reinterpret_cast<uint32_t *>(&sh.hist);
+        for (int i = threadIdx.x; i < static_cast<int>(sizeof(sh.hist) / 4); i += kGivenThreads) all[i] = 0u;
         __syncthreads();
         // addresses less what the first bin's bits come to
         const uint32_t at_n = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.n)) - 4u * kFirstBits;
-        const uint32_t at_low = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.low[(threadIdx.x >> 5) & 1])) - 4u * kFirstBits;
-        uint32_t tail = 0, number = 0;
-        for (uint32_t j = threadIdx.x; j < row.vectors; j += kGivenThreads) {
-            const uint4 w = row.slice[j];
+        const uint32_t at_low = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.low[(threadIdx.x >> 5) % kCopies])) - 4u * kFirstBits;
+        unsigned long long tail = 0;
+        uint32_t number = 0;
+        row.each([&](const uint4 &w, uint32_t) {
+            uint32_t some = 0;                           // of 8 weights of 25 bits
 #pragma unroll
-            for (int i = 0; i < Row<DTYPE>::VEC; i += 2) {
-                const Pair y = log2_of(Row<DTYPE>::values(w, i));
+            for (int i = 0; i < ROW::VEC; i += 2) {
+                const Pair y = log2_of(ROW::values(w, i));
                 float yy[2];
                 uint32_t v[2];
                 of_pair(y, yy[0], yy[1]);
@@ -369,11 +451,12 @@ class Cluster {
                     add_if(binned, at_n + four_bin, 1u);
                     add_if(binned, at_low + four_bin, u & ((1u << kLowBits) - 1u));
                     const uint32_t whole = binned ? 0u : __float2uint_rz(__uint_as_float(u));
-                    tail += whole;
+                    some += whole;
                     number += whole != 0u;
                 }
             }
-        }
+            tail += some;
+        });
         // n and weight of the tail to the first CTA
         Sums total;
         block_before(tail, number, sh.scan, total);
@@ -395,7 +478,8 @@ class Cluster {
             for (uint32_t r = 0; r < kMaxParts; ++r) {       // unrolled: the loads from other SMs overlap
                 if (r >= parts) break;
                 n += *at(&sh.hist.n[bin], r);
-                low += static_cast<unsigned long long>(*at(&sh.hist.low[0][bin], r)) + *at(&sh.hist.low[1][bin], r);
+#pragma unroll
+                for (int k = 0; k < kCopies; ++k) low += *at(&sh.hist.low[k][bin], r);
             }
             const uint32_t v = (bin + kFirstBits) << kLowBits;       // the bin's least weight
             *at(&sh.bins.n[bin], 0) = n;
@@ -405,33 +489,33 @@ class Cluster {
         sync();
     }
 
-    // f(value, column, weight's bits, distance) for the candidates that a command names.
+    // f(column, weight's bits, distance) for the candidates that a command names.
     template <typename F>
     __device__ __forceinline__ void each_named(const Command &c, F f) const {
-        constexpr int VEC = Row<DTYPE>::VEC;
+        constexpr int VEC = ROW::VEC;
         // log2 of the bins' ends, with a margin for the rounding of y and of the logarithm
         const float from = c.bin_lo == kTail ? rw.lowest
                                              : fmaxf(rw.lowest, __log2f(__uint_as_float((c.bin_lo + kFirstBits) << kLowBits)) - 40.01f);
         const float to = __log2f(__uint_as_float((c.bin_hi + 1 + kFirstBits) << kLowBits)) - 39.99f;
-        for (uint32_t j = threadIdx.x; j < row.vectors; j += kGivenThreads) {
-            const uint4 w = row.slice[j];
+        row.each([&](const uint4 &w, uint32_t j) {
             uint32_t hits = 0;
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) {
                 float y0, y1;
-                of_pair(log2_of(Row<DTYPE>::values(w, i)), y0, y1);
+                of_pair(log2_of(ROW::values(w, i)), y0, y1);
                 if (y0 >= from && y0 <= to) hits |= 1u << i;
                 if (y1 >= from && y1 <= to) hits |= 2u << i;
             }
-            while (hits) {
-                const int i = __ffs(hits) - 1;
-                hits &= hits - 1u;
-                const float x = Row<DTYPE>::value(row.slice[j], i);
+            if (!hits) return;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                if (!(hits >> i & 1u)) continue;
+                const float x = ROW::value(w, i);
                 const uint32_t v = power(rw.log2_of(x)), dist = distance(x);
                 const int bin = bin_of(v);
                 if (bin >= c.bin_lo && bin <= c.bin_hi && dist >= c.dist_lo && dist <= c.dist_hi) f(row.col0 + j * VEC + i, v, dist);
             }
-        }
+        });
     }
 
     __device__ __forceinline__ void obey(const Command &c) const {
@@ -480,15 +564,15 @@ class Cluster {
             }
         } else {
             // candidates of one value, in the order of their columns: a run of vectors per thread
-            constexpr int VEC = Row<DTYPE>::VEC;
+            constexpr int VEC = ROW::VEC;
             const float x = __uint_as_float(order_decode(rw.code_m - c.dist_lo));
             const uint32_t run = (row.vectors + kGivenThreads - 1) / kGivenThreads;
             const uint32_t begin = min(threadIdx.x * run, row.vectors), end = min(begin + run, row.vectors);
             uint32_t mine = 0;
             for (uint32_t j = begin; j < end; ++j) {
-                const uint4 w = row.slice[j];
+                const uint4 w = row.vector(j);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) mine += Row<DTYPE>::value(w, i) == x;
+                for (int i = 0; i < VEC; ++i) mine += ROW::value(w, i) == x;
             }
             Sums total;
             const uint32_t before = block_before(0ull, mine, sh.scan, total).n;
@@ -497,10 +581,10 @@ class Cluster {
             } else if (c.part == part && before <= c.which && c.which < before + mine) {
                 uint32_t left = c.which - before;
                 for (uint32_t j = begin; j < end; ++j) {
-                    const uint4 w = row.slice[j];
-#pragma unroll 1
+                    const uint4 w = row.vector(j);
+#pragma unroll
                     for (int i = 0; i < VEC; ++i)
-                        if (Row<DTYPE>::value(w, i) == x && left-- == 0u) *at(&sh.tie_col, 0) = row.col0 + j * VEC + i;
+                        if (ROW::value(w, i) == x && left-- == 0u) *at(&sh.tie_col, 0) = row.col0 + j * VEC + i;
                 }
             }
         }
@@ -532,11 +616,11 @@ struct Found {
 };
 
 // First CTA: the row's bins, scanned, and the list that was made last.
-template <int DTYPE>
+template <typename ROW>
 class Finder {
     static constexpr int kOwn = kBins / kGivenThreads, kOwnFine = kFine / kGivenThreads, kOwnList = kListCap / kGivenThreads;
-    const Cluster<DTYPE> &cl;
-    GivenShared &sh;
+    const Cluster<ROW> &cl;
+    typename ROW::Shared &sh;
     uint32_t own_n0;                       // before this thread's bins (which run from the last down)
     unsigned long long own_w0;
     uint32_t bins_n;                       // of all bins but the tail
@@ -550,7 +634,7 @@ class Finder {
     uint32_t total_n;
     unsigned long long total_w;
 
-    __device__ __forceinline__ explicit Finder(const Cluster<DTYPE> &c) : cl(c), sh(c.sh) {
+    __device__ __forceinline__ explicit Finder(const Cluster<ROW> &c) : cl(c), sh(c.sh) {
         unsigned long long w = 0;
         uint32_t n = 0;
 #pragma unroll
@@ -573,7 +657,7 @@ class Finder {
     }
 
     // The first candidate at which the running number (by_weight false) or weight reaches target, 1 .. the total.
-    __device__ __noinline__ Found find(bool by_weight, unsigned long long target) {
+    __device__ __forceinline__ Found find(bool by_weight, unsigned long long target) {
         const bool listed = by_weight ? target > list_w0 && target <= list_w0 + list_w
                                       : target > list_n0 && target <= static_cast<unsigned long long>(list_n0) + list_n;
         if (!listed) {
@@ -763,161 +847,527 @@ class Finder {
     }
 };
 
-template <int DTYPE, int SCHEME>
-__global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) given_kernel(const GivenArgs a) {
-    constexpr int VEC = Row<DTYPE>::VEC;
-    extern __shared__ __align__(16) uint8_t given_smem[];
-    __shared__ GivenShared sh;
-    uint4 *const slice = reinterpret_cast<uint4 *>(given_smem);
-    const int64_t row = blockIdx.x / a.parts;
-    const uint32_t part = blockIdx.x % a.parts;
+// ---- a row by its weights -------------------------------------------------------------------
+
+// What a row asks for.
+struct Settings {
+    float c, lowest;           // as in RowWeights
+    int64_t top_k;             // 0: off
+    uint64_t p32;              // 0: off
+    uint32_t u32;
+    Settings() = default;
+    __device__ __forceinline__ Settings(const GivenArgs &a, int64_t row) {
+        const float tau = a.temperature[row];
+        const bool greedy = !(tau >= 1e-6f);
+        c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
+        lowest = -40.0f;                                 // below that a weight is 0
+        if (!greedy && a.min_p && a.min_p[row] > 0.0f)
+            lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -40.0f), 0.0f);
+        top_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+        p32 = 0;
+        if (!greedy && a.top_p && a.top_p[row] < 1.0f) {
+            const double p = floor(static_cast<double>(a.top_p[row]) * 4294967296.0);
+            p32 = p >= 1.0 ? static_cast<uint64_t>(p) : 1ull;
+        }
+        const double u = static_cast<double>(a.uniforms[row]) * 4294967296.0;
+        u32 = u >= 4294967295.0 ? 0xffffffffu : u >= 1.0 ? static_cast<uint32_t>(u) : 0u;
+    }
+};
+
+// The three questions in turn: ask(by_weight, target) finds the candidate at which the running number or weight reaches
+// the target; the first two leave the running number and weight up to it.  The last answer is what is drawn.
+template <typename F>
+__device__ __forceinline__ void narrow(const Settings &set, uint32_t &kept, unsigned long long &total, F ask) {
+#pragma unroll 1
+    for (int question = 0; question < 3; ++question) {
+        bool rest;
+        unsigned long long target;
+        if (question == 0) {
+            if (set.top_k <= 0 || set.top_k >= kept) continue;
+            target = static_cast<unsigned long long>(set.top_k);
+        } else if (question == 1) {
+            if (!set.p32) continue;
+            target = share_of(set.p32, total, rest);
+            target += rest;
+            if (target >= total) continue;
+        } else {
+            target = share_of(set.u32, total, rest) + 1ull;
+        }
+        uint32_t n;
+        unsigned long long w;
+        ask(question != 0, target, n, w);
+        if (question < 2) {
+            kept = n;
+            total = w;
+        }
+    }
+}
+
+__device__ __forceinline__ void answer(const GivenArgs &a, int64_t row, uint32_t kept, unsigned long long own, unsigned long long total) {
+    if (a.out_prob) a.out_prob[row] = total ? static_cast<float>(static_cast<double>(own) / static_cast<double>(total)) : 0.0f;
+    if (a.out_kept) a.out_kept[row] = static_cast<int32_t>(kept);
+}
+
+// The whole of a row whose CTAs have all begun.
+template <typename ROW>
+__device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint32_t part, uint8_t *smem) {
+    auto &sh = *reinterpret_cast<typename ROW::Shared *>(smem);
+    constexpr size_t kShared = (sizeof(typename ROW::Shared) + 15) / 16 * 16;
+    ROW r(a, row, part, reinterpret_cast<uint4 *>(smem + kShared));
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (a.parts > 1) cg::this_cluster().barrier_arrive();
-
-    // the row's vectors start at the 16-byte boundary at or before it
-    const uintptr_t row_at = reinterpret_cast<uintptr_t>(a.logits) + static_cast<uintptr_t>(row * a.ld) * (16 / VEC);
-    const uint32_t head = static_cast<uint32_t>(row_at % 16) / (16 / VEC);
-    const uint32_t row_vectors = (head + static_cast<uint32_t>(a.V) + VEC - 1) / VEC;
-    const uint32_t vec0 = min(part * a.part_vectors, row_vectors);
-    const uint32_t vectors = min(a.part_vectors, row_vectors - vec0);
-
-    float m = load_slice<DTYPE, SCHEME>(a, row, slice, vec0, vectors, head);
+    float m = r.load();
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if (lane == 0) sh.warp_max[warp] = m;
     __syncthreads();
+    for (int w = 0; w < kGivenWarps; ++w) m = fmaxf(m, sh.warp_max[w]);
     if (a.parts > 1) {
-        cg::this_cluster().barrier_wait();               // every CTA has begun: its shared memory can be written
-        if (threadIdx.x < a.parts) {
-            for (int w = 1; w < kGivenWarps; ++w) m = fmaxf(m, sh.warp_max[w]);
-            m = fmaxf(m, sh.warp_max[0]);
-            cg::this_cluster().map_shared_rank(sh.part_max, threadIdx.x)[part] = m;
-        }
+        if (threadIdx.x < a.parts) cg::this_cluster().map_shared_rank(sh.part_max, threadIdx.x)[part] = m;
         cg::this_cluster().sync();
-        m = sh.part_max[0];
-        for (uint32_t r = 1; r < a.parts; ++r) m = fmaxf(m, sh.part_max[r]);
-    } else {
-        for (int w = 0; w < kGivenWarps; ++w) m = fmaxf(m, sh.warp_max[w]);
+        for (uint32_t i = 0; i < a.parts; ++i) m = fmaxf(m, sh.part_max[i]);
     }
     if (m == -INFINITY) {                                // nothing can be drawn: every CTA of the cluster sees it
         if (part == 0 && threadIdx.x == 0) {
-            a.out_tokens[row] = 0;
-            if (a.out_prob) a.out_prob[row] = 0.0f;
-            if (a.out_kept) a.out_kept[row] = 0;
+            a.out_tokens[r.row] = 0;
+            answer(a, r.row, 0u, 0ull, 0ull);
         }
         return;
     }
-    if (m == INFINITY) {                                 // the infinite ones share everything
-        for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) {
-            uint32_t *e = reinterpret_cast<uint32_t *>(&slice[j]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (DTYPE == SBW_DTYPE_F32) {
-                    e[i] = e[i] == 0x7f800000u ? 0u : 0xff800000u;
-                } else {
-                    e[i] = ((e[i] & 0xffffu) == 0x7f80u ? 0u : 0xff80u) | ((e[i] >> 16) == 0x7f80u ? 0u : 0xff800000u);
-                }
-            }
-        }
+    if (m == INFINITY) {
+        r.keep_infinite();
         __syncthreads();
         m = 0.0f;
     }
-
-    // the row's settings
-    const float tau = a.temperature[row];
-    const bool greedy = !(tau >= 1e-6f);
+    const Settings set(a, r.row);
     RowWeights rw;
     rw.m = m;
     rw.code_m = order_code(__float_as_uint(m));
-    rw.c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
-    rw.lowest = -40.0f;                                  // below that a weight is 0
-    if (!greedy && a.min_p && a.min_p[row] > 0.0f)
-        rw.lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -40.0f), 0.0f);
-
-    Row<DTYPE> r;
-    r.slice = slice;
-    r.vectors = vectors;
-    r.col0 = vec0 * VEC - head;
-    const Cluster<DTYPE> cl(sh, r, rw, a.parts, part);
+    rw.c = set.c;
+    rw.lowest = set.lowest;
+    const Cluster<ROW> cl(sh, r, rw, a.parts, part);
     cl.histogram();
     cl.merge();
     if (part != 0) {
         cl.serve();
         return;
     }
-    Finder<DTYPE> finder(cl);
-    const int64_t k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+    Finder<ROW> finder(cl);
     uint32_t kept = finder.total_n;
     unsigned long long total = finder.total_w;
-    if (k > 0 && k < kept) {
-        const Found f = finder.find(false, static_cast<unsigned long long>(k));
-        kept = f.n;
-        total = f.running;
-    }
-    if (!greedy && a.top_p && a.top_p[row] < 1.0f) {
-        const double p = floor(static_cast<double>(a.top_p[row]) * 4294967296.0);
-        bool rest;
-        unsigned long long need = share_of(p >= 1.0 ? static_cast<unsigned long long>(p) : 1ull, total, rest);
-        need += rest;
-        if (need < total) {
-            const Found f = finder.find(true, need);
-            kept = f.n;
-            total = f.running;
-        }
-    }
-    const double u = static_cast<double>(a.uniforms[row]) * 4294967296.0;
-    const unsigned long long u32 = u >= 4294967295.0 ? 0xffffffffull : u >= 1.0 ? static_cast<unsigned long long>(u) : 0ull;
-    bool rest;
-    const Found f = finder.find(true, share_of(u32, total, rest) + 1ull);
+    Found f;
+    narrow(set, kept, total, [&](bool by_weight, unsigned long long t, uint32_t &n, unsigned long long &w) {
+        f = finder.find(by_weight, t);
+        n = f.n;
+        w = f.running;
+    });
     if (threadIdx.x == 0) {
-        a.out_tokens[row] = static_cast<int32_t>(f.col);
-        if (a.out_prob) a.out_prob[row] = static_cast<float>(static_cast<double>(f.own) / static_cast<double>(total));
-        if (a.out_kept) a.out_kept[row] = static_cast<int32_t>(kept);
+        a.out_tokens[r.row] = static_cast<int32_t>(f.col);
+        answer(a, r.row, kept, f.own, total);
     }
     Command done = {};
     cl.order(done);
 }
 
+template <int DTYPE, int SCHEME>
+__global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) given_kernel(const GivenArgs a) {
+    using R = Row<DTYPE, SCHEME, true>;
+    extern __shared__ __align__(16) uint8_t given_smem[];
+    if (a.parts > 1) cg::this_cluster().sync();          // every CTA has begun: its shared memory can be written
+    by_weights<R>(a, blockIdx.x / a.parts, blockIdx.x % a.parts, given_smem);
+}
+
+// Out of line, so that what it holds does not weigh on the kernel that hardly ever calls it.
+template <typename ROW>
+__device__ __noinline__ void by_weights_rare(const GivenArgs &a, int64_t row, uint32_t part, uint8_t *smem) {
+    by_weights<ROW>(a, row, part, smem);
+}
+
+// ---- bf16: a row by its values --------------------------------------------------------------
+
+// A bf16 row has few distinct values, so candidates are counted by value: one pass over the row, before its maximum is
+// known, and one add per element; everything else happens on the counters.  The counters are the values of magnitude
+// 2^-56 to 256, of either sign; the ends stand for what lies beyond them as well, zero included (so low a magnitude
+// leaves the differences from the maximum and so the weights as zero does, unless the maximum is about as small).  Rows
+// with a value from 256 on, rows in which values from -256 down have a weight, rows with a maximum below 2^-20 and rows
+// whose token is one of several different values around zero are done by their weights instead.  A second pass finds the
+// column of the value that was drawn.
+constexpr uint32_t kCodes = 8192;                        // magnitudes per sign
+constexpr uint32_t kFirstCode = (71u << 7) + 1u;         // the bits of the smallest magnitude, which is 2^-56 (1 + 2^-7)
+static_assert(2 * kCodes == 32 * kGivenThreads, "a thread per block of 32 places");
+struct CodesShared {
+    uint32_t n[2 * kCodes];                              // positive ones by magnitude, then negative ones
+    unsigned long long block_weight[2 * kCodes / 32];    // of 32 places
+    uint32_t block_n[2 * kCodes / 32];
+    uint32_t warp_best[kGivenWarps], part_best[kMaxParts];
+    Settings set;
+    ScanSlots scan;
+    // what the first CTA tells the others
+    uint32_t by_weights, value, which, around_zero;
+    uint32_t tiny;                                       // some value around zero is not zero
+    // a question
+    unsigned long long weight_before, running, own;
+    uint32_t block, n_before, found_n, found_value, found_which, found_all;
+    uint32_t warp_ties[kGivenWarps], part_ties[kMaxParts];
+};
+
+// In the order of candidates the positive values come first, in blocks of 32 places.  Bits of the fp32 value of place o
+// (zero for the smallest of either sign), and its counter.
+__device__ __forceinline__ uint32_t value_of_place(uint32_t o) {
+    return o - (kCodes - 1) < 2u ? 0u : (o < kCodes ? kFirstCode + (kCodes - 1 - o) : 0x8000u + kFirstCode + (o - kCodes)) << 16;
+}
+__device__ __forceinline__ uint32_t counter_of_place(uint32_t o) { return o < kCodes ? kCodes - 1 - o : o; }
+
+template <int SCHEME>
+__global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) given_codes_kernel(const GivenArgs a) {
+    using R = Row<SBW_DTYPE_BF16, SCHEME, false>;
+    extern __shared__ __align__(16) uint8_t given_smem[];
+    CodesShared &sh = *reinterpret_cast<CodesShared *>(given_smem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t part = blockIdx.x % a.parts;
+    R r(a, blockIdx.x / a.parts, part, nullptr);
+    const auto sync = [&] {
+        if (a.parts > 1) cg::this_cluster().sync();
+        else __syncthreads();
+    };
+    for (uint32_t i = threadIdx.x; i < 2 * kCodes / 4; i += kGivenThreads) reinterpret_cast<uint4 *>(sh.n)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x == 0) sh.tiny = 0u;
+    __syncthreads();
+    // the settings take fp64 divisions and a logarithm: one warp's time, beside the others' loads
+    if (part == 0 && warp == kGivenWarps - 1) {
+        const Settings set(a, r.row);
+        if (lane == 0) sh.set = set;
+    }
+
+    __nv_bfloat162 largest = __floats2bfloat162_rn(-256.0f, -256.0f);
+    const __nv_bfloat162 smallest = __halves2bfloat162(__ushort_as_bfloat16(kFirstCode), __ushort_as_bfloat16(kFirstCode));
+    const uint32_t counters = static_cast<uint32_t>(__cvta_generic_to_shared(sh.n));
+    r.each_loaded([&](const uint4 &w, uint32_t) {
+        const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // two values at a time: NaN and what is below -256 to -256, magnitudes to the counters' range
+            const __nv_bfloat162 x = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&e[i]), __floats2bfloat162_rn(-256.0f, -256.0f));
+            const __nv_bfloat162 size = __hmin2(__hmax2(__habs2(x), smallest), __floats2bfloat162_rn(256.0f, 256.0f));
+            largest = __hmax2(largest, x);
+            // 13 bits of magnitude and the sign above them, twice, as offsets in bytes
+            const uint32_t both = ((*reinterpret_cast<const uint32_t *>(&size) - kFirstCode * 0x10001u) |
+                                   (*reinterpret_cast<const uint32_t *>(&x) >> 2 & 0x20002000u)) << 2;
+            count_one(counters + (both & 0xffffu));
+            count_one(counters + (both >> 16));
+        }
+    });
+    // order code of the largest value (-0 counts as +0)
+    uint32_t best = order_code(__float_as_uint(fmaxf(__low2float(largest), __high2float(largest)) + 0.0f));
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (lane == 0) sh.warp_best[warp] = best;
+    sync();
+    if (a.parts > 1) {
+        // a CTA adds up a share of the counters over all CTAs, in the first one's place: nobody else touches them
+        const uint32_t share = 2 * kCodes / a.parts;     // 4 counters for each of a thread's trips
+        uint4 *const first = reinterpret_cast<uint4 *>(cg::this_cluster().map_shared_rank(sh.n, 0) + part * share);
+        for (uint32_t i = threadIdx.x; i < share / 4; i += kGivenThreads) {
+            uint4 n = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (uint32_t q = 0; q < kMaxParts; ++q) {
+                if (q >= a.parts) break;
+                const uint4 x = reinterpret_cast<const uint4 *>(cg::this_cluster().map_shared_rank(sh.n, q) + part * share)[i];
+                n.x += x.x;
+                n.y += x.y;
+                n.z += x.z;
+                n.w += x.w;
+            }
+            first[i] = n;
+        }
+        if (threadIdx.x < kGivenWarps) {
+            best = __reduce_max_sync((1u << kGivenWarps) - 1u, sh.warp_best[threadIdx.x]);
+            if (threadIdx.x == 0) {
+                cg::this_cluster().map_shared_rank(sh.part_best, 0)[part] = best;
+            }
+        }
+        cg::this_cluster().sync();
+    }
+
+    if (part == 0) {
+        const Settings set = sh.set;
+        if (a.parts > 1) {
+            for (uint32_t i = 0; i < a.parts; ++i) best = max(best, sh.part_best[i]);
+        } else {
+            for (int i = 0; i < kGivenWarps; ++i) best = max(best, sh.warp_best[i]);
+        }
+        RowWeights rw;
+        rw.m = __uint_as_float(order_decode(best));
+        rw.c = set.c;
+        rw.lowest = set.lowest;
+        // values beyond the counters that matter
+        const bool beyond = rw.m >= 256.0f || fabsf(rw.m) < 0x1p-20f || rw.m <= -256.0f ||
+                            (sh.n[2 * kCodes - 1] != 0u && rw.log2_of(-256.0f) >= rw.lowest);
+        if (beyond) {
+            if (threadIdx.x < a.parts) {
+                uint32_t *const flag = &sh.by_weights;
+                *(a.parts > 1 ? cg::this_cluster().map_shared_rank(flag, threadIdx.x) : flag) = 1u;
+            }
+        } else {
+            const auto weight = [&](uint32_t value) -> unsigned long long {
+                const float y = rw.log2_of(__uint_as_float(value));
+                return y >= rw.lowest ? weight_of(power(y)) : 0ull;
+            };
+            // weights of the blocks, a warp per block and a lane per value
+            constexpr int kBlocks = kGivenThreads / kGivenWarps, kAtOnce = 8;
+#pragma unroll 1
+            for (int i0 = 0; i0 < kBlocks; i0 += kAtOnce) {
+                uint32_t num[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) num[i] = sh.n[counter_of_place(((i0 + i) * kGivenWarps + warp) * 32 + lane)];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const uint32_t block = (i0 + i) * kGivenWarps + warp;
+                    unsigned long long w = 0;
+                    uint32_t n = 0;
+                    if (__any_sync(0xffffffffu, num[i] != 0u)) {
+                        w = weight(value_of_place(block * 32 + lane));
+                        n = __reduce_add_sync(0xffffffffu, w ? num[i] : 0u);
+                        w *= num[i];                     // below 2^60: three sums of 20 bits
+                        w = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w) & 0xfffffu) +
+                            (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 20) & 0xfffffu)) << 20) +
+                            (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 40))) << 40);
+                    }
+                    if (lane == 0) {
+                        sh.block_weight[block] = w;
+                        sh.block_n[block] = n;
+                    }
+                }
+            }
+            __syncthreads();
+            const unsigned long long sum_w = sh.block_weight[threadIdx.x];
+            const uint32_t sum_n = sh.block_n[threadIdx.x];
+            Sums all;
+            const Sums before = block_before(sum_w, sum_n, sh.scan, all);
+            // the value at which a target is reached: its block, then a lane per value
+            const auto find = [&](bool by_weight, unsigned long long target, uint32_t &found_n, unsigned long long &running) {
+                if (by_weight ? before.weight < target && target <= before.weight + sum_w
+                              : before.n < target && target <= before.n + static_cast<unsigned long long>(sum_n)) {
+                    sh.block = threadIdx.x;
+                    sh.weight_before = before.weight;
+                    sh.n_before = before.n;
+                }
+                __syncthreads();
+                if (warp == 0) {
+                    const uint32_t place = sh.block * 32 + lane;
+                    const uint32_t value = value_of_place(place);
+                    const unsigned long long w = weight(value);
+                    const uint32_t num = w ? sh.n[counter_of_place(place)] : 0u;
+                    unsigned long long w_to = w * num;
+                    uint32_t n_to = num;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const unsigned long long up = __shfl_up_sync(0xffffffffu, w_to, d);
+                        const uint32_t up_n = __shfl_up_sync(0xffffffffu, n_to, d);
+                        if (lane >= d) {
+                            w_to += up;
+                            n_to += up_n;
+                        }
+                    }
+                    w_to += sh.weight_before;
+                    n_to += sh.n_before;
+                    const unsigned long long w_from = w_to - w * num;
+                    const uint32_t n_from = n_to - num;
+                    if (num && (by_weight ? w_from < target && target <= w_to : n_from < target && target <= n_to)) {
+                        const uint32_t j = static_cast<uint32_t>(by_weight ? (target - w_from + w - 1) / w : target - n_from);
+                        // zeros of either sign are equal
+                        const uint32_t zeros = sh.n[0] + sh.n[kCodes];
+                        sh.found_which = place == kCodes ? j + sh.n[0] : j;
+                        sh.found_value = value;
+                        sh.found_all = value ? num : zeros;
+                        sh.found_n = n_from + j;
+                        sh.running = w_from + w * j;
+                        sh.own = w;
+                    }
+                }
+                __syncthreads();
+                found_n = sh.found_n;
+                running = sh.running;
+            };
+            uint32_t kept = all.n;
+            unsigned long long total = all.weight;
+            narrow(set, kept, total, find);
+            if (threadIdx.x < a.parts) {
+                const auto tell = [&](uint32_t *p, uint32_t x) { *(a.parts > 1 ? cg::this_cluster().map_shared_rank(p, threadIdx.x) : p) = x; };
+                tell(&sh.by_weights, 0u);
+                tell(&sh.value, sh.found_value);
+                tell(&sh.which, sh.found_all == 1u ? 0u : sh.found_which);
+                // of values around zero the first CTA only knows how many there are, not that they are equal
+                tell(&sh.around_zero, sh.found_value == 0u);
+            }
+            if (threadIdx.x == 0) answer(a, r.row, kept, sh.own, total);
+        }
+    }
+    sync();
+    if (!sh.by_weights && sh.around_zero) {
+        // by their weights if one of them is not zero
+        uint32_t tiny = 0;
+        r.each_loaded([&](const uint4 &w, uint32_t) {
+            const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t size = (e[i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+                tiny |= size != 0u && size <= kFirstCode;
+            }
+        });
+        if (__syncthreads_or(static_cast<int>(tiny)) && threadIdx.x < a.parts) {
+            uint32_t *const flag = &sh.tiny;
+            *(a.parts > 1 ? cg::this_cluster().map_shared_rank(flag, threadIdx.x) : flag) = 1u;
+        }
+        sync();
+    }
+    if (sh.by_weights || sh.tiny) {
+        __syncthreads();                                 // the flag has been read: its place is used for other things
+        if (a.parts > 1) cg::this_cluster().sync();
+        by_weights_rare<R>(a, r.row, part, given_smem);
+        return;
+    }
+
+    // The column: of `which` (from 1 on; 0: the only one) among those of the value, a run of vectors per warp.
+    const uint32_t value = sh.value, which = sh.which;
+    const uint32_t bits = value >> 16 | value;           // both halves
+    const __nv_bfloat162 wanted = *reinterpret_cast<const __nv_bfloat162 *>(&bits);
+    const auto equal = [&](uint32_t w) { return __heq2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&w), wanted); };
+    // one bit per element of vector j that has the value
+    const auto hits_of = [&](uint4 w, uint32_t j) -> uint32_t {
+        uint32_t *const e = reinterpret_cast<uint32_t *>(&w);
+        if (!r.whole(j)) {
+            w = r.ragged(j);
+        } else if constexpr (SCHEME != kSchemeNone) {
+            // neither as it is nor with the bias: nothing to hash
+            const uint32_t both = a.bias.delta_bf16 | a.bias.delta_bf16 << 16;
+            uint32_t near = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) near |= equal(e[i]) | equal(add_bf16x2(e[i], both));
+            if (!near) return 0u;
+            bias_vector<SBW_DTYPE_BF16, SCHEME>(w, r.rs, a.vocab_offset + r.col0 + j * R::VEC, a.bias);
+        }
+        uint32_t hits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t m = equal(e[i]);
+            hits |= (m & 1u) << (2 * i) | (m >> 31) << (2 * i + 1);
+        }
+        return hits;
+    };
+    constexpr uint32_t kAtOnce = SCHEME == kSchemeNone ? 8 : 4;
+    const uint32_t run = (r.vectors + 32 * kGivenWarps - 1) / (32 * kGivenWarps) * 32;      // of a warp, whole trips
+    const uint32_t begin = min(warp * run, r.vectors), end = min(begin + run, r.vectors);
+    uint32_t mine = 0;
+    for (uint32_t j0 = begin + lane; j0 < end; j0 += 32 * kAtOnce) {
+        uint4 w[kAtOnce];
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            const uint32_t j = j0 + 32 * u;
+            w[u] = j < end && r.whole(j) ? r.raw(j) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAtOnce; ++u) {
+            const uint32_t j = j0 + 32 * u;
+            if (j >= end) break;
+            const uint32_t hits = hits_of(w[u], j);
+            if (!hits) continue;
+            mine += __popc(hits);
+            if (which == 0u) a.out_tokens[r.row] = static_cast<int32_t>(r.col0 + j * R::VEC + __ffs(hits) - 1);
+        }
+    }
+    if (which == 0u) return;
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) sh.warp_ties[warp] = mine;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+    for (int i = 0; i < kGivenWarps; ++i) {
+        if (i < warp) before += sh.warp_ties[i];
+        total += sh.warp_ties[i];
+    }
+    if (a.parts > 1) {
+        if (threadIdx.x < a.parts) cg::this_cluster().map_shared_rank(sh.part_ties, threadIdx.x)[part] = total;
+        cg::this_cluster().sync();
+        for (uint32_t q = 0; q < part; ++q) before += sh.part_ties[q];
+    }
+    if (which <= before || which > before + mine) return;
+    uint32_t left = which - before;                      // from 1 on, among the warp's
+    for (uint32_t j0 = begin; j0 < end; j0 += 32) {
+        const uint32_t j = j0 + lane;
+        const uint32_t hits = j < end ? hits_of(r.whole(j) ? r.raw(j) : make_uint4(0u, 0u, 0u, 0u), j) : 0u;
+        const uint32_t own = __popc(hits);
+        uint32_t to = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xffffffffu, to, d);
+            if (lane >= d) to += up;
+        }
+        const uint32_t all = __shfl_sync(0xffffffffu, to, 31);
+        if (left > all) {
+            left -= all;
+            continue;
+        }
+        if (to - own < left && left <= to)
+            a.out_tokens[r.row] = static_cast<int32_t>(r.col0 + j * R::VEC + __fns(hits, 0, static_cast<int>(left - (to - own))));
+        break;
+    }
+}
+
 // ---- host -----------------------------------------------------------------------------------
 
-template <int DTYPE, int SCHEME>
-int launch_given(GivenArgs &a, int64_t B, cudaStream_t stream) {
-    constexpr int VEC = Row<DTYPE>::VEC;
-    DeviceInfo di;
-    if (int rc = current_device_info(&di)) return rc;
-    // CTAs per row: so many that two of them fit on an SM (one row's passes over shared memory then run
-    // beside another row's loads), and more where few rows would leave SMs without work
-    const int64_t row_vectors = (a.V + 2 * (VEC - 1)) / VEC;
-    int64_t parts = 1;
-    while (parts < kMaxParts && (row_vectors * 16 > parts * kSliceBytes || (B * parts * 2 <= di.sm_count && row_vectors > parts * kGivenThreads)))
-        parts *= 2;
-    a.parts = static_cast<uint32_t>(parts);
-    a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
-    if (B > 0x7fffffffLL / parts) return SBW_ERR_UNSUPPORTED;
-    const size_t bytes = static_cast<size_t>(a.part_vectors) * 16;
-    const auto kernel = given_kernel<DTYPE, SCHEME>;
-    static std::atomic<uint64_t> prepared{0};
+template <typename K>
+int launch_row_clusters(K kernel, const GivenArgs &a, int64_t B, size_t bytes, int most_bytes, std::atomic<uint64_t> &prepared,
+                        const DeviceInfo &di, cudaStream_t stream) {
+    if (B > 0x7fffffffLL / a.parts) return SBW_ERR_UNSUPPORTED;
     if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
-        // the most that V, up to its limit, asks of a CTA
-        constexpr int64_t kLargest = (kMaxGivenV + 2 * VEC) / VEC * 16 / kMaxParts + 16;
-        constexpr int kMost = static_cast<int>(kLargest > kSliceBytes + 16 ? kLargest : kSliceBytes + 16);
-        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_bytes));
         prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(B * parts));
+    cfg.gridDim = dim3(static_cast<unsigned>(B * a.parts));
     cfg.blockDim = dim3(kGivenThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+    attr[0].val.clusterDim.x = a.parts;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.numAttrs = a.parts > 1 ? 1 : 0;
     SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return SBW_OK;
+}
+
+template <int DTYPE, int SCHEME>
+int launch_given(GivenArgs &a, int64_t B, cudaStream_t stream) {
+    DeviceInfo di;
+    if (int rc = current_device_info(&di)) return rc;
+    if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> prepared{0};
+    constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
+    const int64_t row_vectors = (a.V + 2 * (VEC - 1)) / VEC;
+    int64_t parts = 1;
+    if constexpr (DTYPE == SBW_DTYPE_BF16) {
+        // one CTA per row unless that leaves SMs without work
+        using Shared = typename Row<DTYPE, SCHEME, false>::Shared;
+        constexpr int kBytes = static_cast<int>(sizeof(Shared) > sizeof(CodesShared) ? sizeof(Shared) : sizeof(CodesShared));
+        while (parts < kMaxParts && B * parts <= di.sm_count && row_vectors > parts * kGivenThreads) parts *= 2;
+        a.parts = static_cast<uint32_t>(parts);
+        a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
+        return launch_row_clusters(given_codes_kernel<SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
+    } else {
+        // CTAs per row: so many that two of them fit on an SM (one row's passes over shared memory then run
+        // beside another row's loads), and more where few rows would leave SMs without work
+        using Shared = typename Row<DTYPE, SCHEME, true>::Shared;
+        constexpr size_t kShared = (sizeof(Shared) + 15) / 16 * 16;
+        // the most that V, up to its limit, asks of a CTA
+        constexpr int64_t kLargest = (kMaxGivenV + 2 * VEC) / VEC * 16 / kMaxParts + 16;
+        constexpr int kMost = static_cast<int>(kShared + (kLargest > kSliceBytes + 16 ? kLargest : kSliceBytes + 16));
+        while (parts < kMaxParts && (row_vectors * 16 > parts * kSliceBytes || (B * parts * 2 <= di.sm_count && row_vectors > parts * kGivenThreads)))
+            parts *= 2;
+        a.parts = static_cast<uint32_t>(parts);
+        a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
+        return launch_row_clusters(given_kernel<DTYPE, SCHEME>, a, B, kShared + static_cast<size_t>(a.part_vectors) * 16, kMost, prepared, di, stream);
+    }
 }
 
 }  // namespace

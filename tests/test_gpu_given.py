@@ -153,3 +153,61 @@ def test_rows_of_any_alignment(dtype):
                 x.copy_(inputs.logits_normal(6, V, 2.0, dtype, seed=start))
                 u, tau, k, p, low = settings(6, V + start)
                 compare(x, u, tau, k, p, low)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_values_of_every_size(dtype):
+    """Values from 256 on and from -256 down, magnitudes around 2^-24 and below, zeros of both signs, powers of two."""
+    require_gpu()
+    V = 9000
+    g = torch.Generator().manual_seed(3)
+    n = torch.randn(V, generator=g)
+    rows = [n * 300, n * 0.01 - 300, n * 2.0 ** -24, n * 2.0 ** -30, n * 1e-38, torch.where(n < 0, n, -0.0 * n), n.clone(), n.clone(),
+            n.clone(), n * 100, torch.exp2((n * 8).round()) * torch.sign(n), n * 0 + 255.0, n * 0 - 255.0]
+    rows[6][100], rows[7][5], rows[8][2000:] = 256.0, 2.0 ** -24, -1000.0
+    x = torch.stack(rows).to(dtype).cuda()
+    B = len(rows)
+    for seed in range(3):
+        r = np.random.default_rng(seed)
+        u = r.random(B, dtype=np.float32)
+        for tau in (1.0, 30.0, 1000.0, 0.01):
+            t = np.full(B, tau, np.float32)
+            compare(x, u, t)
+            compare(x, u, t, k=r.integers(1, V, B), p=r.random(B, dtype=np.float32), low=np.full(B, 1e-4))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_any_number_of_rows(dtype):
+    """The numbers of CTAs per row: few rows, as many as SMs, more."""
+    require_gpu()
+    for B in (1, 2, 17, 36, 37, 74, 75, 148, 149, 400):
+        x = inputs.logits_normal(B, 9001, 2.0, dtype, seed=B).cuda()
+        u, tau, k, p, low = settings(B, B)
+        compare(x, u, tau, k, p, low)
+        compare(x, u, np.ones(B, np.float32))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_values_around_zero(dtype):
+    """Draws and cuts among zeros of both signs and magnitudes too small for a counter of their own."""
+    require_gpu()
+    V = 6000
+    g = torch.Generator().manual_seed(8)
+    sign = torch.randint(0, 2, (V,), generator=g) * 2.0 - 1.0
+    low = torch.where(torch.rand(V, generator=g) < 0.3, -5.0 - torch.rand(V, generator=g), 0.0)
+    tiny = torch.exp2(-50.0 - torch.randint(0, 60, (V,), generator=g).float())
+    rows = [low + 0.0 * sign, torch.where(low == 0, 0.0 * sign, low), torch.where(low == 0, tiny * sign, low),
+            torch.where(torch.rand(V, generator=g) < 0.01, tiny * sign, torch.where(low == 0, 0.0 * sign, low))]
+    rows += [r.clone() for r in rows]
+    for i, r in enumerate(rows):
+        r[7] = 0.5 if i < 4 else 2.0 ** -21             # the maximum
+    x = torch.stack(rows).to(dtype).repeat(1, 3).cuda()
+    for seed in range(5):
+        r = np.random.default_rng(seed)
+        u = r.random(len(rows), dtype=np.float32)
+        one = np.ones(len(rows), np.float32)
+        compare(x, u, one)
+        compare(x, u, one, k=r.integers(1, V, len(rows)), p=r.random(len(rows), dtype=np.float32))
+    wide = x[:4].repeat(60, 1)                          # a CTA per row
+    u = np.random.default_rng(9).random(240, dtype=np.float32)
+    compare(wide, u, np.ones(240, np.float32))
