@@ -89,6 +89,31 @@ struct ScanSlots {
     unsigned long long weight[kGivenWarps];
     uint32_t n[kGivenWarps];
 };
+// What a row asks for.
+struct Settings {
+    float c, lowest;           // as in RowWeights
+    int64_t top_k;             // 0: off
+    uint64_t p32;              // 0: off
+    uint32_t u32;
+    Settings() = default;
+    __device__ __forceinline__ Settings(const GivenArgs &a, int64_t row) {
+        const float tau = a.temperature[row];
+        const bool greedy = !(tau >= 1e-6f);
+        c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
+        lowest = -40.0f;                                 // below that a weight is 0
+        if (!greedy && a.min_p && a.min_p[row] > 0.0f)
+            lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -40.0f), 0.0f);
+        top_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+        p32 = 0;
+        if (!greedy && a.top_p && a.top_p[row] < 1.0f) {
+            const double p = floor(static_cast<double>(a.top_p[row]) * 4294967296.0);
+            p32 = p >= 1.0 ? static_cast<uint64_t>(p) : 1ull;
+        }
+        const double u = static_cast<double>(a.uniforms[row]) * 4294967296.0;
+        u32 = u >= 4294967295.0 ? 0xffffffffu : u >= 1.0 ? static_cast<uint32_t>(u) : 0u;
+    }
+};
+
 template <int COPIES>
 struct GivenShared {
     struct {
@@ -116,6 +141,7 @@ struct GivenShared {
     uint32_t found_n_before, found_n;
     uint32_t found_dist, found_col;
     float warp_max[kGivenWarps];
+    Settings set;
     Command cmd;
 };
 
@@ -154,27 +180,39 @@ __device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) {
 // weights of sbw_bias_sample_filtered, the latter times 2^40: a power of two changes no rounding.  The weight is what
 // truncation leaves of it.
 constexpr float kRound = 12582912.0f;                // 1.5 2^23: the last bits of y + kRound are rint(y)
-__device__ __forceinline__ void power(Pair y, uint32_t &v0, uint32_t &v1) {
-    const Pair t = pair_add(y, pair_of(kRound, kRound));
-    const Pair f = pair_fma(pair_add(t, pair_of(-kRound, -kRound)), pair_of(-1.0f, -1.0f), y);
-    Pair p = pair_of(0x1.ffcbfcp+23f, 0x1.ffcbfcp+23f);
-    p = pair_fma(p, f, pair_of(0x1.430912p+27f, 0x1.430912p+27f));
-    p = pair_fma(p, f, pair_of(0x1.5d87fep+30f, 0x1.5d87fep+30f));
-    p = pair_fma(p, f, pair_of(0x1.3b2ab6p+33f, 0x1.3b2ab6p+33f));
-    p = pair_fma(p, f, pair_of(0x1.c6b08ep+35f, 0x1.c6b08ep+35f));
-    p = pair_fma(p, f, pair_of(0x1.ebfbep+37f, 0x1.ebfbep+37f));
-    p = pair_fma(p, f, pair_of(0x1.62e43p+39f, 0x1.62e43p+39f));
-    p = pair_fma(p, f, pair_of(0x1p+40f, 0x1p+40f));
-    float p0, p1, t0, t1;
-    of_pair(p, p0, p1);
-    of_pair(t, t0, t1);
-    v0 = __float_as_uint(p0) + (__float_as_uint(t0) << 23);      // the low bits of kRound are 0: n goes to the exponent
-    v1 = __float_as_uint(p1) + (__float_as_uint(t1) << 23);
+// N pairs side by side: a step's constant, which takes two registers, is made once for all of them.
+template <int N>
+__device__ __forceinline__ void power(const Pair (&y)[N], uint32_t (&v)[2 * N]) {
+    constexpr float kSteps[7] = {0x1.430912p+27f, 0x1.5d87fep+30f, 0x1.3b2ab6p+33f, 0x1.c6b08ep+35f, 0x1.ebfbep+37f, 0x1.62e43p+39f, 0x1p+40f};
+    Pair t[N], f[N], p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = pair_add(y[i], pair_of(kRound, kRound));
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = pair_add(t[i], pair_of(-kRound, -kRound));
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = pair_fma(f[i], pair_of(-1.0f, -1.0f), y[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = pair_of(0x1.ffcbfcp+23f, 0x1.ffcbfcp+23f);
+#pragma unroll
+    for (int k = 0; k < 7; ++k) {
+        const Pair c = pair_of(kSteps[k], kSteps[k]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = pair_fma(p[i], f[i], c);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float p0, p1, t0, t1;
+        of_pair(p[i], p0, p1);
+        of_pair(t[i], t0, t1);
+        v[2 * i] = __float_as_uint(p0) + (__float_as_uint(t0) << 23);      // the low bits of kRound are 0: n goes to the exponent
+        v[2 * i + 1] = __float_as_uint(p1) + (__float_as_uint(t1) << 23);
+    }
 }
 __device__ __forceinline__ uint32_t power(float y) {
-    uint32_t v, other;
-    power(pair_of(y, y), v, other);
-    return v;
+    const Pair one[1] = {pair_of(y, y)};
+    uint32_t v[2];
+    power(one, v);
+    return v[0];
 }
 __device__ __forceinline__ int bin_of(uint32_t v) {
     const int b = static_cast<int>(v >> kLowBits) - static_cast<int>(kFirstBits);
@@ -360,6 +398,19 @@ struct Row {
         if (infinite) only_infinite<DTYPE>(w);
         return w;
     }
+    // Element i of vector j, which is one of the row's.
+    __device__ __forceinline__ float value_at(uint32_t j, int i) const {
+        float x;
+        if constexpr (RESIDENT) {
+            x = DTYPE == SBW_DTYPE_F32 ? reinterpret_cast<const float *>(slice + j)[i]
+                                       : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(slice + j)[i]);
+        } else {
+            const uint32_t col = col0 + j * VEC + i;
+            x = fmaxf(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias) + 0.0f, -INFINITY);
+            if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
+        }
+        return x;
+    }
     // Brings a resident part in; returns the thread's largest value.
     __device__ __forceinline__ float load() {
         float best = -INFINITY;
@@ -388,11 +439,14 @@ struct Row {
 __device__ __forceinline__ void count_one(uint32_t addr) {
     asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], %1;" ::"r"(addr), "r"(1u) : "memory");
 }
-// One add to shared memory under a condition, as a predicated instruction: a branch per element would keep the
-// elements of a vector from overlapping.
-__device__ __forceinline__ void add_if(bool yes, uint32_t addr, uint32_t x) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.relaxed.cta.shared::cta.add.u32 [%0], %1;\n\t}"
-                 ::"r"(addr), "r"(x), "r"(static_cast<uint32_t>(yes)) : "memory");
+// One candidate of weight u (fp32 bits; 0: none) in the histogram, at counters n and low, or its truncation `whole` to the
+// tail.  Predicated: a branch per element would keep the elements of a vector from overlapping.
+__device__ __forceinline__ void weigh_one(uint32_t u, uint32_t n, uint32_t low, uint32_t whole, uint32_t &tail) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ge.u32 p, %1, %2;\n\t"
+                 "@p red.relaxed.cta.shared::cta.add.u32 [%3], 1;\n\t"
+                 "@p red.relaxed.cta.shared::cta.add.u32 [%4], %5;\n\t"
+                 "@!p add.u32 %0, %0, %6;\n\t}"
+                 : "+r"(tail) : "r"(u), "r"(kFirstBits << kLowBits), "r"(n), "r"(low), "r"(u & ((1u << kLowBits) - 1u)), "r"(whole) : "memory");
 }
 
 template <typename ROW>
@@ -433,58 +487,65 @@ class Cluster {
         const uint32_t at_n = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.n)) - 4u * kFirstBits;
         const uint32_t at_low = static_cast<uint32_t>(__cvta_generic_to_shared(sh.hist.low[(threadIdx.x >> 5) % kCopies])) - 4u * kFirstBits;
         unsigned long long tail = 0;
-        uint32_t number = 0;
+        uint32_t number = 0;                             // of all candidates
         row.each([&](const uint4 &w, uint32_t) {
+            constexpr int VEC = ROW::VEC;
             uint32_t some = 0;                           // of 8 weights of 25 bits
+            Pair y[VEC / 2];
+            uint32_t v[VEC];
 #pragma unroll
-            for (int i = 0; i < ROW::VEC; i += 2) {
-                const Pair y = log2_of(ROW::values(w, i));
+            for (int i = 0; i < VEC / 2; ++i) y[i] = log2_of(ROW::values(w, 2 * i));
+            power(y, v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
                 float yy[2];
-                uint32_t v[2];
-                of_pair(y, yy[0], yy[1]);
-                power(y, v[0], v[1]);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t u = yy[k] >= rw.lowest ? v[k] : 0u;
-                    const bool binned = u >= kFirstBits << kLowBits;
-                    const uint32_t four_bin = u >> (kLowBits - 2) & ~3u;
-                    add_if(binned, at_n + four_bin, 1u);
-                    add_if(binned, at_low + four_bin, u & ((1u << kLowBits) - 1u));
-                    const uint32_t whole = binned ? 0u : __float2uint_rz(__uint_as_float(u));
-                    some += whole;
-                    number += whole != 0u;
-                }
+                of_pair(y[i / 2], yy[0], yy[1]);
+                const bool real = yy[i & 1] >= rw.lowest;
+                const uint32_t u = real ? v[i] : 0u;
+                number += real;
+                weigh_one(u, at_n + 4u * (u >> kLowBits), at_low + 4u * (u >> kLowBits), __float2uint_rz(__uint_as_float(u)), some);
             }
             tail += some;
         });
-        // n and weight of the tail to the first CTA
         Sums total;
-        block_before(tail, number, sh.scan, total);
+        block_before(tail, number, sh.scan, total);      // its barriers also end the histogram
+        // the bins' weights
+        uint32_t binned = 0;
+#pragma unroll
+        for (int k = 0; k < kBins / kGivenThreads; ++k) {
+            const uint32_t bin = k * kGivenThreads + threadIdx.x, n = sh.hist.n[bin], v = (bin + kFirstBits) << kLowBits;
+            unsigned long long low = static_cast<unsigned long long>(n) * ((v & 0x7fffffu) | 0x800000u);
+#pragma unroll
+            for (int q = 0; q < kCopies; ++q) low += sh.hist.low[q][bin];
+            sh.bins.n[bin] = n;
+            sh.bins.weight[bin] = low << shift_of_bin(static_cast<int>(bin));
+            binned += n;
+        }
+        Sums total_binned;
+        block_before(0ull, binned, sh.scan, total_binned);
         if (threadIdx.x == 0) {
             at(sh.tail_weight, 0)[part] = total.weight;
-            at(sh.tail_n, 0)[part] = total.n;
+            at(sh.tail_n, 0)[part] = total.n - total_binned.n;
         }
     }
 
-    // Every CTA adds up a share of the bins over all CTAs and hands it to the first.
+    // Every CTA adds up a share of the bins over all CTAs, in the first one's place: nobody else touches them.
     __device__ __forceinline__ void merge() const {
         sync();
-        const uint32_t share = kBins / parts;            // a power of two
-        for (uint32_t i = threadIdx.x; i < share; i += kGivenThreads) {
-            const uint32_t bin = part * share + i;
+        if (parts == 1) return;
+        const uint32_t share = kBins / parts;            // a power of two, at most one bin per thread
+        if (threadIdx.x < share) {
+            const uint32_t bin = part * share + threadIdx.x;
             uint32_t n = 0;
-            unsigned long long low = 0;
+            unsigned long long w = 0;
 #pragma unroll
             for (uint32_t r = 0; r < kMaxParts; ++r) {       // unrolled: the loads from other SMs overlap
                 if (r >= parts) break;
-                n += *at(&sh.hist.n[bin], r);
-#pragma unroll
-                for (int k = 0; k < kCopies; ++k) low += *at(&sh.hist.low[k][bin], r);
+                n += *at(&sh.bins.n[bin], r);
+                w += *at(&sh.bins.weight[bin], r);
             }
-            const uint32_t v = (bin + kFirstBits) << kLowBits;       // the bin's least weight
             *at(&sh.bins.n[bin], 0) = n;
-            *at(&sh.bins.weight[bin], 0) =
-                (static_cast<unsigned long long>(n) * ((v & 0x7fffffu) | 0x800000u) + low) << shift_of_bin(static_cast<int>(bin));
+            *at(&sh.bins.weight[bin], 0) = w;
         }
         sync();
     }
@@ -495,8 +556,8 @@ class Cluster {
         constexpr int VEC = ROW::VEC;
         // log2 of the bins' ends, with a margin for the rounding of y and of the logarithm
         const float from = c.bin_lo == kTail ? rw.lowest
-                                             : fmaxf(rw.lowest, __log2f(__uint_as_float((c.bin_lo + kFirstBits) << kLowBits)) - 40.01f);
-        const float to = __log2f(__uint_as_float((c.bin_hi + 1 + kFirstBits) << kLowBits)) - 39.99f;
+                                             : fmaxf(rw.lowest, __log2f(__uint_as_float((c.bin_lo + kFirstBits) << kLowBits)) - 40.001f);
+        const float to = __log2f(__uint_as_float((c.bin_hi + 1 + kFirstBits) << kLowBits)) - 39.999f;
         row.each([&](const uint4 &w, uint32_t j) {
             uint32_t hits = 0;
 #pragma unroll
@@ -506,11 +567,12 @@ class Cluster {
                 if (y0 >= from && y0 <= to) hits |= 1u << i;
                 if (y1 >= from && y1 <= to) hits |= 2u << i;
             }
-            if (!hits) return;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                if (!(hits >> i & 1u)) continue;
-                const float x = ROW::value(w, i);
+            // few: their values are fetched again, which keeps this loop's body small
+#pragma unroll 1
+            while (hits) {
+                const int i = __ffs(hits) - 1;
+                hits &= hits - 1u;
+                const float x = row.value_at(j, i);
                 const uint32_t v = power(rw.log2_of(x)), dist = distance(x);
                 const int bin = bin_of(v);
                 if (bin >= c.bin_lo && bin <= c.bin_hi && dist >= c.dist_lo && dist <= c.dist_hi) f(row.col0 + j * VEC + i, v, dist);
@@ -849,31 +911,6 @@ class Finder {
 
 // ---- a row by its weights -------------------------------------------------------------------
 
-// What a row asks for.
-struct Settings {
-    float c, lowest;           // as in RowWeights
-    int64_t top_k;             // 0: off
-    uint64_t p32;              // 0: off
-    uint32_t u32;
-    Settings() = default;
-    __device__ __forceinline__ Settings(const GivenArgs &a, int64_t row) {
-        const float tau = a.temperature[row];
-        const bool greedy = !(tau >= 1e-6f);
-        c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
-        lowest = -40.0f;                                 // below that a weight is 0
-        if (!greedy && a.min_p && a.min_p[row] > 0.0f)
-            lowest = fminf(fmaxf(static_cast<float>(log2(static_cast<double>(a.min_p[row]))), -40.0f), 0.0f);
-        top_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-        p32 = 0;
-        if (!greedy && a.top_p && a.top_p[row] < 1.0f) {
-            const double p = floor(static_cast<double>(a.top_p[row]) * 4294967296.0);
-            p32 = p >= 1.0 ? static_cast<uint64_t>(p) : 1ull;
-        }
-        const double u = static_cast<double>(a.uniforms[row]) * 4294967296.0;
-        u32 = u >= 4294967295.0 ? 0xffffffffu : u >= 1.0 ? static_cast<uint32_t>(u) : 0u;
-    }
-};
-
 // The three questions in turn: ask(by_weight, target) finds the candidate at which the running number or weight reaches
 // the target; the first two leave the running number and weight up to it.  The last answer is what is drawn.
 template <typename F>
@@ -915,6 +952,10 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
     constexpr size_t kShared = (sizeof(typename ROW::Shared) + 15) / 16 * 16;
     ROW r(a, row, part, reinterpret_cast<uint4 *>(smem + kShared));
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (part == 0 && warp == kGivenWarps - 1) {
+        const Settings set(a, row);
+        for (uint32_t i = lane; i < a.parts; i += 32) *(a.parts > 1 ? cg::this_cluster().map_shared_rank(&sh.set, i) : &sh.set) = set;
+    }
     float m = r.load();
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -938,7 +979,7 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
         __syncthreads();
         m = 0.0f;
     }
-    const Settings set(a, r.row);
+    const Settings set = sh.set;
     RowWeights rw;
     rw.m = m;
     rw.code_m = order_code(__float_as_uint(m));
@@ -968,9 +1009,14 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
     cl.order(done);
 }
 
+// fp32 rows.  Plain ones are read again from L2 by every pass, a CTA per row if there are as many rows as SMs (256 x 151936:
+// 330 us with the row resident in the shared memory of a cluster, which then waits for its first CTA); watermarked ones are
+// resident, since the hash costs more than a pass.
+template <int DTYPE, int SCHEME>
+using RowOf = Row<DTYPE, SCHEME, SCHEME != kSchemeNone>;
 template <int DTYPE, int SCHEME>
 __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) given_kernel(const GivenArgs a) {
-    using R = Row<DTYPE, SCHEME, true>;
+    using R = RowOf<DTYPE, SCHEME>;
     extern __shared__ __align__(16) uint8_t given_smem[];
     if (a.parts > 1) cg::this_cluster().sync();          // every CTA has begun: its shared memory can be written
     by_weights<R>(a, blockIdx.x / a.parts, blockIdx.x % a.parts, given_smem);
@@ -1112,29 +1158,29 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
                 return y >= rw.lowest ? weight_of(power(y)) : 0ull;
             };
             // weights of the blocks, a warp per block and a lane per value
-            constexpr int kBlocks = kGivenThreads / kGivenWarps, kAtOnce = 8;
+            uint32_t some = 0;                           // which of the warp's 32 have candidates
+#pragma unroll 8
+            for (int i = 0; i < 32; ++i) {
+                const bool any = __any_sync(0xffffffffu, sh.n[counter_of_place((i * kGivenWarps + warp) * 32 + lane)] != 0u);
+                some |= static_cast<uint32_t>(any) << i;
+            }
+            sh.block_weight[lane * kGivenWarps + warp] = 0ull;
+            sh.block_n[lane * kGivenWarps + warp] = 0u;
+            __syncwarp();
 #pragma unroll 1
-            for (int i0 = 0; i0 < kBlocks; i0 += kAtOnce) {
-                uint32_t num[kAtOnce];
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) num[i] = sh.n[counter_of_place(((i0 + i) * kGivenWarps + warp) * 32 + lane)];
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) {
-                    const uint32_t block = (i0 + i) * kGivenWarps + warp;
-                    unsigned long long w = 0;
-                    uint32_t n = 0;
-                    if (__any_sync(0xffffffffu, num[i] != 0u)) {
-                        w = weight(value_of_place(block * 32 + lane));
-                        n = __reduce_add_sync(0xffffffffu, w ? num[i] : 0u);
-                        w *= num[i];                     // below 2^60: three sums of 20 bits
-                        w = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w) & 0xfffffu) +
-                            (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 20) & 0xfffffu)) << 20) +
-                            (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 40))) << 40);
-                    }
-                    if (lane == 0) {
-                        sh.block_weight[block] = w;
-                        sh.block_n[block] = n;
-                    }
+            while (some) {
+                const uint32_t block = (__ffs(some) - 1) * kGivenWarps + warp;
+                some &= some - 1u;
+                const uint32_t num = sh.n[counter_of_place(block * 32 + lane)];
+                unsigned long long w = weight(value_of_place(block * 32 + lane));
+                const uint32_t n = __reduce_add_sync(0xffffffffu, w ? num : 0u);
+                w *= num;                                // below 2^60: three sums of 20 bits
+                w = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w) & 0xfffffu) +
+                    (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 20) & 0xfffffu)) << 20) +
+                    (static_cast<unsigned long long>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(w >> 40))) << 40);
+                if (lane == 0) {
+                    sh.block_weight[block] = w;
+                    sh.block_n[block] = n;
                 }
             }
             __syncthreads();
@@ -1346,18 +1392,18 @@ int launch_given(GivenArgs &a, int64_t B, cudaStream_t stream) {
     constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
     const int64_t row_vectors = (a.V + 2 * (VEC - 1)) / VEC;
     int64_t parts = 1;
-    if constexpr (DTYPE == SBW_DTYPE_BF16) {
+    if constexpr (DTYPE == SBW_DTYPE_BF16 || SCHEME == kSchemeNone) {
         // one CTA per row unless that leaves SMs without work
         using Shared = typename Row<DTYPE, SCHEME, false>::Shared;
         constexpr int kBytes = static_cast<int>(sizeof(Shared) > sizeof(CodesShared) ? sizeof(Shared) : sizeof(CodesShared));
         while (parts < kMaxParts && B * parts <= di.sm_count && row_vectors > parts * kGivenThreads) parts *= 2;
         a.parts = static_cast<uint32_t>(parts);
         a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
-        return launch_row_clusters(given_codes_kernel<SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
+        if constexpr (DTYPE == SBW_DTYPE_BF16) return launch_row_clusters(given_codes_kernel<SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
+        else return launch_row_clusters(given_kernel<DTYPE, SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
     } else {
-        // CTAs per row: so many that two of them fit on an SM (one row's passes over shared memory then run
-        // beside another row's loads), and more where few rows would leave SMs without work
-        using Shared = typename Row<DTYPE, SCHEME, true>::Shared;
+        // CTAs per row: as many as its slices need, and more where few rows would leave SMs without work
+        using Shared = typename RowOf<DTYPE, SCHEME>::Shared;
         constexpr size_t kShared = (sizeof(Shared) + 15) / 16 * 16;
         // the most that V, up to its limit, asks of a CTA
         constexpr int64_t kLargest = (kMaxGivenV + 2 * VEC) / VEC * 16 / kMaxParts + 16;
