@@ -36,8 +36,10 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kMaxStages = 16;
 constexpr int kTmemColumns = 512;
 constexpr uint64_t kWaitLimit = 2000000000ull;      // nanoseconds
-constexpr int kStageWords = 32 * 33;                // a warp's staging area for stores: 32 rows of 32 words, padded
-constexpr int kStagingBytes = kEpilogueWarps * kStageWords * 4;
+constexpr int kRowWords = 64;                        // of a row that go through the staging area at a time
+constexpr int kRowStride = kRowWords + 2;            // 8-byte accesses by row and by column without bank conflicts; the
+                                                     // two words behind a row hold its watermark seed
+constexpr int kStagingBytes = kTileM * kRowStride * 4;
 constexpr int kMaxDynamicBytes = 227 * 1024 - 1024;  // what a CTA can have less the barriers
 
 struct HeadArgs {
@@ -135,6 +137,26 @@ __device__ __forceinline__ void read_done(uint32_t (&r)[32]) {
                    "+r"(r[30]), "+r"(r[31])::"memory");
 }
 
+// Two fp32 operations per instruction.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(uint32_t a, uint32_t b) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(a), "r"(b));
+    return p;
+}
+__device__ __forceinline__ void of_pair(Pair p, uint32_t &a, uint32_t &b) { asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(p)); }
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16_pair(Pair p) {
+    uint32_t a, b;
+    of_pair(p, a, b);
+    const __nv_bfloat162 q = __floats2bfloat162_rn(__uint_as_float(a), __uint_as_float(b));
+    return *reinterpret_cast<const uint32_t *>(&q);
+}
+
 // ---- the epilogue's last step ---------------------------------------------------------------
 
 // A row's seed as it is handed from lane to lane.
@@ -152,37 +174,59 @@ __device__ __forceinline__ void green_words(uint64_t seed, uint32_t vg, const Bi
     rs.template word0_n<N>(vg, p.key, p.weyl, x);
 }
 
-// Writes 32 words (32 fp32 logits, or 64 bf16 ones in pairs) per row of the warp's rows: the words have
-// been laid out in shared memory by row = lane and leave it by column = lane, so that a row is one
-// 128-byte store.
+// Writes 64 words (64 fp32 logits, or 128 bf16 ones in pairs) of each of `rows` rows from the staging area, every warp
+// each eighth row, a lane two words: a row is one 256-byte store.  Words were laid out there by row = lane.  Eight rows are
+// read before the first is stored: the compiler keeps reads behind stores that it cannot tell from them, and one row at a
+// time took 150 clocks a row (2048 x 128256 x 4096: 1.3 of 2.1 ms).  The green test is shared out the same way, so that
+// few rows keep all warps busy.
 template <int DTYPE, int SCHEME>
-__device__ __forceinline__ void store_chunk(const HeadArgs &a, const uint32_t *staged, int rows, int64_t row0, uint32_t col0,
-                                            uint64_t seed, int lane) {
-    constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2;
-    const uint32_t col = col0 + lane * PER;
-    char *const base = static_cast<char *>(a.logits) + (row0 * a.ld + col) * (4 / PER);
-    const int64_t stride = a.ld * (4 / PER);
-    const bool whole = col + PER <= a.V && (PER == 1 || (reinterpret_cast<uintptr_t>(base) % 4 == 0 && stride % 4 == 0));
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-        uint32_t w = staged[r * 33 + lane];
+__device__ __forceinline__ void store_rows(const HeadArgs &a, const uint32_t *staging, int rows, int64_t row0,
+                                           uint32_t col0, int warp, int lane) {
+    constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2, COLS = 2 * PER, ESIZE = 4 / PER, kAtOnce = SCHEME == kSchemeNone ? 8 : 2;
+    const uint32_t col = col0 + lane * COLS;
+    char *const base = static_cast<char *>(a.logits) + (row0 * a.ld + col) * ESIZE;
+    const int64_t stride = a.ld * ESIZE;
+    const bool whole = col + COLS <= a.V && reinterpret_cast<uintptr_t>(base) % 8 == 0 && stride % 8 == 0;
+    for (int r0 = warp; r0 < rows; r0 += kAtOnce * kEpilogueWarps) {
+        uint2 w[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r0 + u * kEpilogueWarps;
+            w[u] = r < rows ? *reinterpret_cast<const uint2 *>(staging + r * kRowStride + 2 * lane) : make_uint2(0u, 0u);
+        }
         if constexpr (SCHEME != kSchemeNone) {
-            uint32_t x[PER];
-            green_words<SCHEME, PER>(__shfl_sync(0xffffffffu, seed, r), a.vocab_offset + col, a.bias, x);
-            if constexpr (DTYPE == SBW_DTYPE_F32) {
-                if (x[0] <= a.bias.thr_m1) w = __float_as_uint(__fadd_rn(__uint_as_float(w), a.bias.delta));
-            } else {
-                w = add_bf16x2(w, (x[0] <= a.bias.thr_m1 ? a.bias.delta_bf16 : 0x8000u) |
-                                      (x[1] <= a.bias.thr_m1 ? a.bias.delta_bf16 << 16 : 0x80000000u));
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int r = r0 + u * kEpilogueWarps;
+                if (r >= rows) break;
+                uint32_t x[COLS];
+                green_words<SCHEME, COLS>(*reinterpret_cast<const uint64_t *>(staging + r * kRowStride + kRowWords), a.vocab_offset + col, a.bias, x);
+                if constexpr (DTYPE == SBW_DTYPE_F32) {
+                    if (x[0] <= a.bias.thr_m1) w[u].x = __float_as_uint(__fadd_rn(__uint_as_float(w[u].x), a.bias.delta));
+                    if (x[1] <= a.bias.thr_m1) w[u].y = __float_as_uint(__fadd_rn(__uint_as_float(w[u].y), a.bias.delta));
+                } else {
+                    const uint32_t lo = a.bias.delta_bf16, hi = a.bias.delta_bf16 << 16;
+                    w[u].x = add_bf16x2(w[u].x, (x[0] <= a.bias.thr_m1 ? lo : 0x8000u) | (x[1] <= a.bias.thr_m1 ? hi : 0x80000000u));
+                    w[u].y = add_bf16x2(w[u].y, (x[2] <= a.bias.thr_m1 ? lo : 0x8000u) | (x[3] <= a.bias.thr_m1 ? hi : 0x80000000u));
+                }
             }
         }
-        char *const at = base + r * stride;
-        if (!SBW_CHECKED(col >= a.V || row0 + r < a.B, SBW_SITE_HEAD_STORE)) continue;
-        if (whole) {
-            *reinterpret_cast<uint32_t *>(at) = w;
-        } else if constexpr (PER == 2) {
-            if (col < a.V) *reinterpret_cast<uint16_t *>(at) = static_cast<uint16_t>(w);
-            if (col + 1 < a.V) *reinterpret_cast<uint16_t *>(at + 2) = static_cast<uint16_t>(w >> 16);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r0 + u * kEpilogueWarps;
+            if (r >= rows || !SBW_CHECKED(row0 + r < a.B, SBW_SITE_HEAD_STORE)) break;
+            char *const at = base + r * stride;
+            if (whole) {
+                *reinterpret_cast<uint2 *>(at) = w[u];
+            } else {
+#pragma unroll
+                for (int i = 0; i < COLS; ++i) {
+                    const uint32_t v = i < PER ? w[u].x : w[u].y;
+                    if (col + i >= a.V) break;
+                    if constexpr (DTYPE == SBW_DTYPE_F32) reinterpret_cast<uint32_t *>(at)[i] = v;
+                    else reinterpret_cast<uint16_t *>(at)[i] = static_cast<uint16_t>(v >> (16 * (i & 1)));
+                }
+            }
         }
     }
 }
@@ -233,7 +277,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const uint32_t tmem = tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
+    // The epilogue's sums take more registers than an even share; the split is the launch's total (168 x 384).
     if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0 && lane == 0) {
             uint32_t stage = 0, parity = 0;
             int64_t issued = 0;
@@ -292,8 +338,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         }
         __syncwarp();
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         const int quarter = warp % 4, half = (warp - 4) / 4;
-        uint32_t *const staged = staging + (warp - 4) * kStageWords;
         uint32_t buf = 0, parity = 0;
         bool ok = true;
         for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
@@ -305,18 +351,36 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             const uint32_t vb = min(col0, a.V - 1) / kBlock;
             const float *const ws = a.ws + static_cast<int64_t>(vb) * a.ld_ws;
             const float *const xs = a.xs + (rows ? row : 0) * a.ld_xs;
-            float acc[HALF];
+            Pair acc[HALF / 2];
 #pragma unroll
-            for (int i = 0; i < HALF; ++i) acc[i] = 0.0f;
-            float next = __ldg(xs) * __ldg(ws);
+            for (int i = 0; i < HALF / 2; ++i) acc[i] = 0ull;
+            // the two scales of the next four blocks are on their way while four are multiplied
+            float sx[4], sw[4], s4[4];
+            const auto fetch = [&](uint32_t first) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t at = min(first + i, a.kblocks - 1);
+                    sx[i] = __ldg(xs + at);
+                    sw[i] = __ldg(ws + at);
+                }
+            };
+            fetch(0);
             for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
-                const float s = next;
-                if (kb + 1 < a.kblocks) next = __ldg(xs + kb + 1) * __ldg(ws + kb + 1);
+                if (kb % 4 == 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s4[i] = sx[i] * sw[i];
+                    fetch(kb + 4);
+                }
+                const float s = s4[0];
+                s4[0] = s4[1];
+                s4[1] = s4[2];
+                s4[2] = s4[3];
                 if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (rows) {
                     const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + half * HALF;
+                    const Pair both = pair_of(__float_as_uint(s), __float_as_uint(s));
                     uint32_t r[2][32];
                     read_columns(r[0], from);
 #pragma unroll
@@ -324,8 +388,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                         read_done(r[c & 1]);
                         if (c + 1 < HALF / 32) read_columns(r[(c + 1) & 1], from + 32 * (c + 1));
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            acc[32 * c + i] = __fmaf_rn(__uint_as_float(r[c & 1][i]), s, acc[32 * c + i]);
+                        for (int i = 0; i < 16; ++i)
+                            acc[16 * c + i] = pair_fma(pair_of(r[c & 1][2 * i], r[c & 1][2 * i + 1]), both, acc[16 * c + i]);
                     }
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -336,28 +400,41 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     parity ^= 1u;
                 }
             }
-            if (!rows) continue;
             if (!ok) {
 #pragma unroll
-                for (int i = 0; i < HALF; ++i) acc[i] = __uint_as_float(0x7fffffffu);
+                for (int i = 0; i < HALF / 2; ++i) acc[i] = ~0ull;           // NaN
             }
-            uint64_t seed = 0;
-            if constexpr (SCHEME != kSchemeNone) seed = row_seed<SCHEME>(a, row);
-            constexpr int CHUNK = DTYPE == SBW_DTYPE_F32 ? 32 : 64;
+            // The sums leave through the staging area, 64 words of a row at a time: a warpgroup's columns, a part of them, or
+            // (bf16, 128 columns) both warpgroups' at once.
+            constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2;
+            constexpr int WORDS = HALF / PER < kRowWords ? HALF / PER : kRowWords;      // of a warpgroup in one pass
+            constexpr int kAlone = HALF / PER / WORDS;                                  // passes of one warpgroup's columns
+            constexpr int kPasses = WORDS < kRowWords ? 1 : 2 * kAlone;
+            const int64_t m0 = (t % a.m_tiles) * kTileM;
+            const int tile_rows = static_cast<int64_t>(a.B) - m0 < kTileM ? static_cast<int>(a.B - m0) : kTileM;
+            if constexpr (SCHEME != kSchemeNone)
+                if (half == 0 && rows)
+                    *reinterpret_cast<uint64_t *>(staging + (quarter * 32 + lane) * kRowStride + kRowWords) = row_seed<SCHEME>(a, row);
 #pragma unroll
-            for (int c = 0; c < HALF / CHUNK; ++c) {
+            for (int pass = 0; pass < kPasses; ++pass) {
+                if (rows && (kPasses == 1 || half == pass / kAlone)) {
+                    uint32_t *const to = staging + (quarter * 32 + lane) * kRowStride + (kPasses == 1 ? half * WORDS : 0);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    if constexpr (DTYPE == SBW_DTYPE_F32) {
-                        staged[lane * 33 + i] = __float_as_uint(acc[CHUNK * c + i]);
-                    } else {
-                        const __nv_bfloat162 p = __floats2bfloat162_rn(acc[CHUNK * c + 2 * i], acc[CHUNK * c + 2 * i + 1]);
-                        staged[lane * 33 + i] = *reinterpret_cast<const uint32_t *>(&p);
+                    for (int i = 0; i < WORDS; i += 2) {
+                        const int c = (kPasses == 1 ? 0 : pass % kAlone) * WORDS + i;
+                        uint2 w;
+                        if constexpr (DTYPE == SBW_DTYPE_F32) {
+                            of_pair(acc[c / 2], w.x, w.y);
+                        } else {
+                            w = make_uint2(bf16_pair(acc[c]), bf16_pair(acc[c + 1]));
+                        }
+                        *reinterpret_cast<uint2 *>(to + i) = w;
                     }
                 }
-                __syncwarp();
-                if (col0 + CHUNK * c < a.V) store_chunk<DTYPE, SCHEME>(a, staged, rows, row0, col0 + CHUNK * c, seed, lane);
-                __syncwarp();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                store_rows<DTYPE, SCHEME>(a, staging, tile_rows, m0, static_cast<uint32_t>(t / a.m_tiles) * BN + pass * kRowWords * PER,
+                                          warp - 4, lane);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
     }
