@@ -52,6 +52,7 @@ struct HeadArgs {
     int64_t tiles;
     uint32_t x_bytes;          // of one stage's block of hidden states
     uint32_t stages;
+    uint32_t strided;          // rows of the logits do not start on 8-byte boundaries
     const int32_t *ctx;
     int W;
     uint32_t vocab_offset;
@@ -116,27 +117,19 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// 32 columns of a warp's 32 lanes; the values may be used after read_done on the same array.
-__device__ __forceinline__ void read_columns(uint32_t (&r)[32], uint32_t addr) {
+// 16 columns of a warp's 32 lanes; the values may be used after read_done on the same array.
+__device__ __forceinline__ void read_columns(uint32_t (&r)[16], uint32_t addr) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
 }
-__device__ __forceinline__ void read_done(uint32_t (&r)[32]) {
+__device__ __forceinline__ void read_done(uint32_t (&r)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
-                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
-                   "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
-                   "+r"(r[30]), "+r"(r[31])::"memory");
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
-
 // Two fp32 operations per instruction.
 using Pair = unsigned long long;
 __device__ __forceinline__ Pair pair_of(uint32_t a, uint32_t b) {
@@ -159,72 +152,127 @@ __device__ __forceinline__ uint32_t bf16_pair(Pair p) {
 
 // ---- the epilogue's last step ---------------------------------------------------------------
 
-// A row's seed as it is handed from lane to lane.
+// What a row's seed takes to make, as one number.
 template <int SCHEME>
 __device__ __forceinline__ uint64_t row_seed(const HeadArgs &a, int64_t row) {
     if constexpr (SCHEME == SBW_SCHEME_CONTEXT) return seed_context(a.bias.key, a.ctx + row * a.W, a.W);
-    else if constexpr (SCHEME == SBW_SCHEME_SELFSALT) return jenkins_min(a.ctx + row * a.W, a.W);
-    else return 0;
+    else return jenkins_min(a.ctx + row * a.W, a.W);
 }
-template <int SCHEME, int N>
-__device__ __forceinline__ void green_words(uint64_t seed, uint32_t vg, const BiasParams &p, uint32_t (&x)[N]) {
-    RowSeedS<SCHEME> rs;
-    if constexpr (SCHEME == SBW_SCHEME_CONTEXT) rs.rk = make_row_keys(seed);
-    else rs.jmin = static_cast<uint32_t>(seed);
-    rs.template word0_n<N>(vg, p.key, p.weyl, x);
-}
+
+// The green tests of a tile, made by the epilogue's warps while they wait for its products: at small B the weights'
+// bytes leave them idle most of the time (64 x 128256 x 4096: 135 us with the tests after the sums).  A warp has every
+// eighth row of the tile and a lane COLS columns of each 64 words of it, next to each other or (strided) 32 apart; a test
+// is one bit.
+template <int DTYPE, int SCHEME, int BN>
+struct Greens {
+    static constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2, COLS = 2 * PER;
+    static constexpr int kRows = kTileM / kEpilogueWarps, kParts = BN / PER / kRowWords;
+    static constexpr int kBits = kRows * kParts * COLS;
+    uint64_t bits[SCHEME == kSchemeNone ? 1 : kBits / 64];
+    uint32_t done, steps;
+
+    __device__ __forceinline__ void begin(int rows, int warp) {
+#pragma unroll
+        for (auto &b : bits) b = 0ull;
+        done = 0u;
+        steps = rows > warp ? static_cast<uint32_t>((rows - warp + kEpilogueWarps - 1) / kEpilogueWarps) * kParts : 0u;
+    }
+    // Up to `most` more: step i is part i % kParts of the warp's row i / kParts, whose seed lies behind its place in the
+    // staging area.
+    __device__ __forceinline__ void advance(const HeadArgs &a, const uint32_t *staging, uint32_t most, uint32_t col0, int warp, int lane) {
+        if constexpr (SCHEME != kSchemeNone) {
+#pragma unroll 1
+            for (; most > 0u && done < steps; --most, ++done) {
+                const uint64_t seed = *reinterpret_cast<const uint64_t *>(staging + (warp + done / kParts * kEpilogueWarps) * kRowStride + kRowWords);
+                RowSeedS<SCHEME> rs;
+                if constexpr (SCHEME == SBW_SCHEME_CONTEXT) rs.rk = make_row_keys(seed);
+                else rs.jmin = static_cast<uint32_t>(seed);
+                const uint32_t first = a.vocab_offset + col0 + done % kParts * (kRowWords * PER);
+                uint32_t x[COLS];
+                if (a.strided) {
+#pragma unroll
+                    for (int i = 0; i < COLS; ++i) x[i] = rs.word0(first + 32 * i + lane, a.bias.key, a.bias.weyl);
+                } else {
+                    rs.template word0_n<COLS>(first + lane * COLS, a.bias.key, a.bias.weyl, x);
+                }
+                uint64_t g = 0;
+#pragma unroll
+                for (int i = 0; i < COLS; ++i) g |= static_cast<uint64_t>(x[i] <= a.bias.thr_m1) << i;
+                const uint32_t at = done * COLS;
+#pragma unroll
+                for (int i = 0; i < kBits / 64; ++i)
+                    if (at / 64 == static_cast<uint32_t>(i)) bits[i] |= g << (at % 64);
+            }
+        }
+    }
+    // Those of part `part` of the warp's row number r.
+    __device__ __forceinline__ uint32_t of(int r, int part) const {
+        const uint32_t at = static_cast<uint32_t>(r * kParts + part) * COLS;
+        uint64_t b = bits[0];
+#pragma unroll
+        for (int i = 1; i < kBits / 64; ++i)
+            if (at / 64 == static_cast<uint32_t>(i)) b = bits[i];
+        return static_cast<uint32_t>(b >> (at % 64));
+    }
+};
 
 // Writes 64 words (64 fp32 logits, or 128 bf16 ones in pairs) of each of `rows` rows from the staging area, every warp
 // each eighth row, a lane two words: a row is one 256-byte store.  Words were laid out there by row = lane.  Eight rows are
 // read before the first is stored: the compiler keeps reads behind stores that it cannot tell from them, and one row at a
-// time took 150 clocks a row (2048 x 128256 x 4096: 1.3 of 2.1 ms).  The green test is shared out the same way, so that
-// few rows keep all warps busy.
-template <int DTYPE, int SCHEME>
-__device__ __forceinline__ void store_rows(const HeadArgs &a, const uint32_t *staging, int rows, int64_t row0,
-                                           uint32_t col0, int warp, int lane) {
-    constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2, COLS = 2 * PER, ESIZE = 4 / PER, kAtOnce = SCHEME == kSchemeNone ? 8 : 2;
-    const uint32_t col = col0 + lane * COLS;
-    char *const base = static_cast<char *>(a.logits) + (row0 * a.ld + col) * ESIZE;
+// time took 150 clocks a row (2048 x 128256 x 4096: 1.3 of 2.1 ms).
+template <int DTYPE, int SCHEME, int BN>
+__device__ __forceinline__ void store_rows(const HeadArgs &a, const uint32_t *staging, const Greens<DTYPE, SCHEME, BN> &greens, int part,
+                                           int rows, int64_t row0, uint32_t col0, int warp, int lane) {
+    constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2, COLS = 2 * PER, ESIZE = 4 / PER, kAtOnce = 8;
+    char *const base = static_cast<char *>(a.logits) + (row0 * a.ld + col0) * ESIZE;
     const int64_t stride = a.ld * ESIZE;
-    const bool whole = col + COLS <= a.V && reinterpret_cast<uintptr_t>(base) % 8 == 0 && stride % 8 == 0;
-    for (int r0 = warp; r0 < rows; r0 += kAtOnce * kEpilogueWarps) {
+#pragma unroll 1
+    for (int i0 = 0; warp + i0 * kEpilogueWarps < rows; i0 += kAtOnce) {
         uint2 w[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int r = r0 + u * kEpilogueWarps;
-            w[u] = r < rows ? *reinterpret_cast<const uint2 *>(staging + r * kRowStride + 2 * lane) : make_uint2(0u, 0u);
+            const int r = warp + (i0 + u) * kEpilogueWarps;
+            const uint32_t *const from = staging + r * kRowStride;
+            if (r >= rows) {
+                w[u] = make_uint2(0u, 0u);
+            } else if (!a.strided) {
+                w[u] = *reinterpret_cast<const uint2 *>(from + 2 * lane);
+            } else if constexpr (DTYPE == SBW_DTYPE_F32) {
+                w[u] = make_uint2(from[lane], from[32 + lane]);
+            } else {
+                const uint16_t *const e = reinterpret_cast<const uint16_t *>(from);
+                w[u] = make_uint2(e[lane] | static_cast<uint32_t>(e[32 + lane]) << 16, e[64 + lane] | static_cast<uint32_t>(e[96 + lane]) << 16);
+            }
         }
         if constexpr (SCHEME != kSchemeNone) {
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
-                const int r = r0 + u * kEpilogueWarps;
-                if (r >= rows) break;
-                uint32_t x[COLS];
-                green_words<SCHEME, COLS>(*reinterpret_cast<const uint64_t *>(staging + r * kRowStride + kRowWords), a.vocab_offset + col, a.bias, x);
+                const uint32_t g = greens.of(i0 + u, part);
                 if constexpr (DTYPE == SBW_DTYPE_F32) {
-                    if (x[0] <= a.bias.thr_m1) w[u].x = __float_as_uint(__fadd_rn(__uint_as_float(w[u].x), a.bias.delta));
-                    if (x[1] <= a.bias.thr_m1) w[u].y = __float_as_uint(__fadd_rn(__uint_as_float(w[u].y), a.bias.delta));
+                    if (g & 1u) w[u].x = __float_as_uint(__fadd_rn(__uint_as_float(w[u].x), a.bias.delta));
+                    if (g & 2u) w[u].y = __float_as_uint(__fadd_rn(__uint_as_float(w[u].y), a.bias.delta));
                 } else {
                     const uint32_t lo = a.bias.delta_bf16, hi = a.bias.delta_bf16 << 16;
-                    w[u].x = add_bf16x2(w[u].x, (x[0] <= a.bias.thr_m1 ? lo : 0x8000u) | (x[1] <= a.bias.thr_m1 ? hi : 0x80000000u));
-                    w[u].y = add_bf16x2(w[u].y, (x[2] <= a.bias.thr_m1 ? lo : 0x8000u) | (x[3] <= a.bias.thr_m1 ? hi : 0x80000000u));
+                    w[u].x = add_bf16x2(w[u].x, (g & 1u ? lo : 0x8000u) | (g & 2u ? hi : 0x80000000u));
+                    w[u].y = add_bf16x2(w[u].y, (g & 4u ? lo : 0x8000u) | (g & 8u ? hi : 0x80000000u));
                 }
             }
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int r = r0 + u * kEpilogueWarps;
+            const int r = warp + (i0 + u) * kEpilogueWarps;
             if (r >= rows || !SBW_CHECKED(row0 + r < a.B, SBW_SITE_HEAD_STORE)) break;
             char *const at = base + r * stride;
-            if (whole) {
-                *reinterpret_cast<uint2 *>(at) = w[u];
+            const uint32_t first = a.strided ? lane : lane * COLS, apart = a.strided ? 32 : 1;
+            if (!a.strided && col0 + first + COLS <= a.V) {
+                *reinterpret_cast<uint2 *>(at + lane * 8) = w[u];
             } else {
 #pragma unroll
                 for (int i = 0; i < COLS; ++i) {
-                    const uint32_t v = i < PER ? w[u].x : w[u].y;
-                    if (col + i >= a.V) break;
-                    if constexpr (DTYPE == SBW_DTYPE_F32) reinterpret_cast<uint32_t *>(at)[i] = v;
-                    else reinterpret_cast<uint16_t *>(at)[i] = static_cast<uint16_t>(v >> (16 * (i & 1)));
+                    const uint32_t v = i < PER ? w[u].x : w[u].y, c = first + i * apart;
+                    if (col0 + c >= a.V) break;
+                    if constexpr (DTYPE == SBW_DTYPE_F32) reinterpret_cast<uint32_t *>(at)[c] = v;
+                    else reinterpret_cast<uint16_t *>(at)[c] = static_cast<uint16_t>(v >> (16 * (i & 1)));
                 }
             }
         }
@@ -234,7 +282,7 @@ __device__ __forceinline__ void store_rows(const HeadArgs &a, const uint32_t *st
 template <int DTYPE, int SCHEME, int BN>
 __global__ void __launch_bounds__(kHeadThreads, 1)
     head_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const HeadArgs a) {
-    constexpr int HALF = BN / 2;                       // columns of one warpgroup of the epilogue
+    constexpr int PART = BN / 2;                       // columns of one warpgroup of the epilogue
     constexpr int NBUF = kTmemColumns / BN;            // accumulators
     constexpr uint32_t kWBytes = BN * kBlock;
     // fp32 accumulator, both operands e4m3 with K along their rows, 128 x BN
@@ -339,62 +387,68 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int quarter = warp % 4, half = (warp - 4) / 4;
+        const int quarter = warp % 4, wg = warp / 4 - 1;
         uint32_t buf = 0, parity = 0;
+        int64_t seeds_of = -1;                           // first row of the tile whose seeds are there
         bool ok = true;
         for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
             const int64_t row0 = (t % a.m_tiles) * kTileM + quarter * 32;
-            const uint32_t col0 = static_cast<uint32_t>(t / a.m_tiles) * BN + half * HALF;
+            const uint32_t col0 = static_cast<uint32_t>(t / a.m_tiles) * BN + wg * PART;
             const int64_t left = static_cast<int64_t>(a.B) - row0;
             const int rows = left < 0 ? 0 : left < 32 ? static_cast<int>(left) : 32;
             const int64_t row = row0 + (lane < rows ? lane : 0);
             const uint32_t vb = min(col0, a.V - 1) / kBlock;
             const float *const ws = a.ws + static_cast<int64_t>(vb) * a.ld_ws;
             const float *const xs = a.xs + (rows ? row : 0) * a.ld_xs;
-            Pair acc[HALF / 2];
-#pragma unroll
-            for (int i = 0; i < HALF / 2; ++i) acc[i] = 0ull;
-            // the two scales of the next four blocks are on their way while four are multiplied
-            float sx[4], sw[4], s4[4];
-            const auto fetch = [&](uint32_t first) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t at = min(first + i, a.kblocks - 1);
-                    sx[i] = __ldg(xs + at);
-                    sw[i] = __ldg(ws + at);
+            const int64_t m0 = (t % a.m_tiles) * kTileM;
+            const int tile_rows = static_cast<int64_t>(a.B) - m0 < kTileM ? static_cast<int>(a.B - m0) : kTileM;
+            const uint32_t tile_col = static_cast<uint32_t>(t / a.m_tiles) * BN;
+            Greens<DTYPE, SCHEME, BN> greens;
+            greens.begin(tile_rows, warp - 4);
+            if constexpr (SCHEME != kSchemeNone) {
+                if (m0 != seeds_of) {                    // the rows' seeds, behind their places in the staging area
+                    if (wg == 0 && rows)
+                        *reinterpret_cast<uint64_t *>(staging + (quarter * 32 + lane) * kRowStride + kRowWords) = row_seed<SCHEME>(a, row);
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    seeds_of = m0;
                 }
-            };
-            fetch(0);
+            }
+            const uint32_t per_block = SCHEME == kSchemeNone ? 0u : (greens.steps + a.kblocks - 1) / a.kblocks;
+            Pair acc[PART / 2];
+#pragma unroll
+            for (int i = 0; i < PART / 2; ++i) acc[i] = 0ull;
+            float sx = __ldg(xs), sw = __ldg(ws);        // a block's scales are on their way while the one before is added
             for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
-                if (kb % 4 == 0) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s4[i] = sx[i] * sw[i];
-                    fetch(kb + 4);
+                const float s = sx * sw;
+                if (kb + 1 < a.kblocks) {
+                    sx = __ldg(xs + kb + 1);
+                    sw = __ldg(ws + kb + 1);
                 }
-                const float s = s4[0];
-                s4[0] = s4[1];
-                s4[1] = s4[2];
-                s4[2] = s4[3];
+                greens.advance(a, staging, per_block, tile_col, warp - 4, lane);
                 if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (rows) {
-                    const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + half * HALF;
-                    const Pair both = pair_of(__float_as_uint(s), __float_as_uint(s));
-                    uint32_t r[2][32];
-                    read_columns(r[0], from);
+                const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + wg * PART;
+                const Pair both = pair_of(__float_as_uint(s), __float_as_uint(s));
+uint32_t r[2][16];
+                if (rows) read_columns(r[0], from);
 #pragma unroll
-                    for (int c = 0; c < HALF / 32; ++c) {
+                for (int c = 0; c < PART / 16; ++c) {
+                    if (rows) {
                         read_done(r[c & 1]);
-                        if (c + 1 < HALF / 32) read_columns(r[(c + 1) & 1], from + 32 * (c + 1));
+                        if (c + 1 < PART / 16) read_columns(r[(c + 1) & 1], from + 16 * (c + 1));
+                    }
+                    if (c + 1 == PART / 16) {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive(taken + 8 * buf);
+                    }
+                    if (rows) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[16 * c + i] = pair_fma(pair_of(r[c & 1][2 * i], r[c & 1][2 * i + 1]), both, acc[16 * c + i]);
+                        for (int i = 0; i < 8; ++i)
+                            acc[8 * c + i] = pair_fma(pair_of(r[c & 1][2 * i], r[c & 1][2 * i + 1]), both, acc[8 * c + i]);
                     }
                 }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) barrier_arrive(taken + 8 * buf);
                 if (++buf == NBUF) {
                     buf = 0;
                     parity ^= 1u;
@@ -402,38 +456,27 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             }
             if (!ok) {
 #pragma unroll
-                for (int i = 0; i < HALF / 2; ++i) acc[i] = ~0ull;           // NaN
+                for (int i = 0; i < PART / 2; ++i) acc[i] = ~0ull;           // NaN
             }
-            // The sums leave through the staging area, 64 words of a row at a time: a warpgroup's columns, a part of them, or
-            // (bf16, 128 columns) both warpgroups' at once.
+            // The sums leave through the staging area, 64 words of a row at a time: all or half of the columns of
+            // one warpgroup, or those of both.
             constexpr int PER = DTYPE == SBW_DTYPE_F32 ? 1 : 2;
-            constexpr int WORDS = HALF / PER < kRowWords ? HALF / PER : kRowWords;      // of a warpgroup in one pass
-            constexpr int kAlone = HALF / PER / WORDS;                                  // passes of one warpgroup's columns
-            constexpr int kPasses = WORDS < kRowWords ? 1 : 2 * kAlone;
-            const int64_t m0 = (t % a.m_tiles) * kTileM;
-            const int tile_rows = static_cast<int64_t>(a.B) - m0 < kTileM ? static_cast<int>(a.B - m0) : kTileM;
-            if constexpr (SCHEME != kSchemeNone)
-                if (half == 0 && rows)
-                    *reinterpret_cast<uint64_t *>(staging + (quarter * 32 + lane) * kRowStride + kRowWords) = row_seed<SCHEME>(a, row);
+            constexpr int kOwnWords = PART / PER, WORDS = kOwnWords < kRowWords ? kOwnWords : kRowWords;
+            constexpr int kTogether = kRowWords / WORDS, kSub = kOwnWords / WORDS, kPasses = 2 * kOwnWords / kRowWords;
 #pragma unroll
             for (int pass = 0; pass < kPasses; ++pass) {
-                if (rows && (kPasses == 1 || half == pass / kAlone)) {
-                    uint32_t *const to = staging + (quarter * 32 + lane) * kRowStride + (kPasses == 1 ? half * WORDS : 0);
+                if (rows && (kTogether > 1 ? wg / kTogether == pass : wg == pass / kSub)) {
+                    uint32_t *const to = staging + (quarter * 32 + lane) * kRowStride + wg % kTogether * WORDS;
 #pragma unroll
                     for (int i = 0; i < WORDS; i += 2) {
-                        const int c = (kPasses == 1 ? 0 : pass % kAlone) * WORDS + i;
                         uint2 w;
-                        if constexpr (DTYPE == SBW_DTYPE_F32) {
-                            of_pair(acc[c / 2], w.x, w.y);
-                        } else {
-                            w = make_uint2(bf16_pair(acc[c]), bf16_pair(acc[c + 1]));
-                        }
+                        if constexpr (DTYPE == SBW_DTYPE_F32) of_pair(acc[(i + pass % kSub * WORDS) / 2], w.x, w.y);
+                        else w = make_uint2(bf16_pair(acc[i + pass % kSub * WORDS]), bf16_pair(acc[i + 1 + pass % kSub * WORDS]));
                         *reinterpret_cast<uint2 *>(to + i) = w;
                     }
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                store_rows<DTYPE, SCHEME>(a, staging, tile_rows, m0, static_cast<uint32_t>(t / a.m_tiles) * BN + pass * kRowWords * PER,
-                                          warp - 4, lane);
+                store_rows<DTYPE, SCHEME, BN>(a, staging, greens, pass, tile_rows, m0, tile_col + pass * kRowWords * PER, warp - 4, lane);
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
         }
@@ -493,6 +536,8 @@ int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     const size_t bytes = 1024 + a.stages * stage_bytes + kStagingBytes;
     a.m_tiles = (a.B + kTileM - 1) / kTileM;
+    constexpr int kEsize = DTYPE == SBW_DTYPE_F32 ? 4 : 2;
+    a.strided = reinterpret_cast<uintptr_t>(a.logits) % 8 != 0 || a.ld * kEsize % 8 != 0;
     a.tiles = static_cast<int64_t>(a.m_tiles) * ((a.V + BN - 1) / BN);
     CUtensorMap map_x, map_w;
     if (int rc = make_map(&map_x, x, a.B, K, ld_x, box_m)) return rc;

@@ -71,3 +71,158 @@ def test_head_is_the_product(B, V, K, dtype):
         assert bool((full[:, V:] == 7).all())
     at_odd = torch.empty(B * V + 1, dtype=dtype, device="cuda")[1:].view(B, V)      # starts on an element, no more
     assert torch.equal(sbw.sbw_head_logits(x, xs, w, ws, at_odd), out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scheme", [0, 1])
+@pytest.mark.parametrize("B,V,K,W,off", [(1, 129, 100, 1, 0), (2, 1000, 256, 4, 7), (64, 515, 128, 1, 0), (100, 257, 640, 8, 2 ** 32 - 257),
+                                         (128, 384, 64, 2, 128), (130, 700, 300, 1, 0), (300, 513, 2048, 4, 1)])
+def test_watermark_on_the_way_out(B, V, K, W, off, scheme, dtype):
+    """The bits of the plain product followed by sbw_bias_logits."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+    from paper_2609_03844_b200 import inputs
+
+    x, w, xs, ws = codes(B, K, 1), codes(V, K, 2), scales(B, K, 3), scales(blocks(V), K, 4)
+    ctx = inputs.uniform_tokens((B, W), V, seed=5).cuda()
+    for ld in (V, V + 1, V + 8):
+        plain, marked = (torch.full((B, ld), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+        sbw.sbw_head_logits(x, xs, w, ws, plain)
+        sbw.sbw_bias_logits(plain, ctx, KEY, 0.25, 2.0, scheme, V=V, vocab_offset=off)
+        sbw.sbw_head_logits(x, xs, w, ws, marked, ctx_tokens=ctx, key=KEY, gamma=0.25, delta=2.0, scheme=scheme, vocab_offset=off)
+        assert_same_bits(host_bits(marked), host_bits(plain))
+    tiny = torch.empty(B, V, dtype=dtype, device="cuda")      # a bias that is 0 in the logits' precision needs no context
+    sbw.sbw_head_logits(x, xs, w, ws, tiny, ctx_tokens=ctx, delta=0.0)
+    assert_same_bits(host_bits(tiny), host_bits(sbw.sbw_head_logits(x, xs, w, ws, torch.empty_like(tiny))))
+
+
+def test_rows_shards_streams_and_captures():
+    """Rows do not depend on each other nor on the batch's size, shards of the vocabulary are slices; calls on several streams
+    and replays of a capture give the same bits."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    B, V, K = 200, 1280, 512
+    x, w, xs, ws = codes(B, K, 1), codes(V, K, 2), scales(B, K, 3), scales(blocks(V), K, 4)
+    all_rows = sbw.sbw_head_logits(x, xs, w, ws, torch.empty(B, V, device="cuda"))
+    for lo, hi in ((0, 1), (5, 70), (100, 200)):
+        part = sbw.sbw_head_logits(x[lo:hi], xs[lo:hi], w, ws, torch.empty(hi - lo, V, device="cuda"))
+        assert torch.equal(part, all_rows[lo:hi])
+    halves = torch.empty(B, V, device="cuda")
+    sbw.sbw_head_logits(x, xs, w[:512], ws[:4], halves[:, :512])
+    sbw.sbw_head_logits(x, xs, w[512:], ws[4:], halves[:, 512:])
+    assert torch.equal(halves, all_rows)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    outs = [torch.empty(B, V, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o in zip(streams, outs):
+            sbw.sbw_head_logits(x, xs, w, ws, o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, all_rows) for o in outs)
+    graph, out, out2 = torch.cuda.CUDAGraph(), torch.empty(B, V, device="cuda"), torch.empty(3, V, dtype=torch.bfloat16, device="cuda")
+    with torch.cuda.graph(graph):
+        sbw.sbw_head_logits(x, xs, w, ws, out)
+        sbw.sbw_head_logits(x[:3], xs[:3], w, ws, out2)
+    for seed in (7, 8):
+        x.copy_(codes(B, K, seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, size = by_definition(x, xs, w, ws)
+        check(out, want, size, K)
+        check(out2, want[:3], size[:3], K)
+
+
+def test_values_that_are_no_numbers():
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    B, V, K = 40, 300, 400
+    x, w, xs, ws = codes(B, K, 1), codes(V, K, 2), scales(B, K, 3), scales(blocks(V), K, 4)
+    want = sbw.sbw_head_logits(x, xs, w, ws, torch.empty(B, V, device="cuda"))
+    x.view(torch.uint8)[3, 399] = 0x7F                        # NaN codes
+    w.view(torch.uint8)[200, 0] = 0xFF
+    xs[5, 1] = float("nan")
+    xs[6, 0] = float("inf")
+    got = sbw.sbw_head_logits(x, xs, w, ws, torch.empty(B, V, device="cuda"))
+    bad = torch.zeros(B, V, dtype=torch.bool, device="cuda")
+    bad[3], bad[5], bad[6], bad[:, 200] = True, True, True, True
+    assert torch.equal(got[~bad], want[~bad])
+    assert bool(got[3].isnan().all() and got[5].isnan().all() and got[:, 200].isnan().all()) and not bool(got[6].isfinite().any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("R,K", [(1, 1), (1, 128), (3, 130), (128, 128), (129, 257), (200, 1000), (1000, 64), (2, 5000), (300, 384)])
+def test_quantizer(R, K, block_rows, dtype):
+    """Scales and codes bit for bit: both divisions are IEEE fp32, which numpy's are, and torch rounds to e4m3 to nearest even."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    g = torch.Generator().manual_seed(R + K)
+    x = (torch.randn(R, K, generator=g) * torch.exp(3 * torch.randn(R, 1, generator=g))).to(dtype)
+    x[0, : K // 2] = 0.0
+    if R > 1:
+        x[1] = 0.0
+        x[R - 1, K - 1] = 2.0 ** -140 if dtype == torch.float32 else 2.0 ** -130
+    pad = lambda n, b: -(-n // b) * b  # noqa: E731
+    full = np.zeros((pad(R, block_rows), pad(K, 128)), np.float32)
+    full[:R, :K] = x.float().numpy()
+    b = full.reshape(-1, block_rows, pad(K, 128) // 128, 128)
+    scale = np.maximum(np.abs(b).max((1, 3)) / np.float32(448), np.float32(2.0 ** -126))
+    q = (b / scale[:, None, :, None]).reshape(full.shape)[:R, :K]
+    want = torch.from_numpy(np.ascontiguousarray(np.clip(q, -448, 448))).to(torch.float8_e4m3fn).view(torch.uint8)
+    for extra in (0, 1, 16):
+        src = torch.full((R, K + extra), float("nan"), dtype=dtype, device="cuda")
+        src[:, :K] = x.cuda()
+        out = torch.full((R, K + extra), 0x55, dtype=torch.uint8, device="cuda")
+        s = torch.full((-(-R // block_rows), blocks(K) + extra), 7.0, device="cuda")
+        sbw.sbw_quantize_fp8(src[:, :K], out.view(E4M3)[:, :K], s[:, :blocks(K)], block_rows=block_rows)
+        assert np.array_equal(s[:, :blocks(K)].cpu().numpy(), scale) and bool((s[:, blocks(K):] == 7).all())
+        assert torch.equal(out[:, :K].cpu(), want) and bool((out[:, K:] == 0x55).all())
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantizer_of_values_that_are_no_numbers(block_rows):
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        x = torch.ones(130, 300, device="cuda")
+        x[2, 140] = bad
+        q, s = torch.empty(130, 300, dtype=E4M3, device="cuda"), torch.empty(-(-130 // block_rows), 3, device="cuda")
+        sbw.sbw_quantize_fp8(x, q, s, block_rows=block_rows)
+        there = torch.zeros(130, 300, dtype=torch.bool, device="cuda")
+        there[2 if block_rows == 1 else slice(0, 128), 128:256] = True
+        back = q.float() * s.repeat_interleave(block_rows, 0)[:130].repeat_interleave(128, 1)[:, :300]
+        assert bool(back[there].isnan().all()) and bool((back[~there] == 1).all())
+
+
+def test_gradient_of_the_hidden_states():
+    """d_x = d_l w is the same product with the transposed weights: against the formula, and against differences of the
+    forward product in 64 bits (which is linear in x)."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    B, V, K = 24, 640, 384
+    g = torch.Generator().manual_seed(4)
+    w = torch.randn(V, K, generator=g).cuda() * 0.02
+    wq, ws = torch.empty(V, K, dtype=E4M3, device="cuda"), torch.empty(blocks(V), blocks(K), device="cuda")
+    sbw.sbw_quantize_fp8(w, wq, ws, block_rows=128)
+    dl = torch.randn(B, V, generator=g).cuda()
+    dq, ds = torch.empty(B, V, dtype=E4M3, device="cuda"), torch.empty(B, blocks(V), device="cuda")
+    sbw.sbw_quantize_fp8(dl, dq, ds)
+    dx = sbw.sbw_head_logits(dq, ds, wq.view(torch.uint8).T.contiguous().view(E4M3), ws.T.contiguous(), torch.empty(B, K, device="cuda"))
+    at = torch.arange(V, device="cuda") // 128
+    W = wq.double() * ws.double()[at][:, torch.arange(K, device="cuda") // 128]
+    D = dq.double() * ds.double()[:, at]
+    check(dx, D @ W, D.abs() @ W.abs(), V)
+    x, step = torch.randn(B, K, generator=g).double().cuda(), torch.randn(B, K, generator=g).double().cuda()
+    loss = lambda v: (D * (v @ W.T)).sum()  # noqa: E731
+    slope = (loss(x + step) - loss(x - step)) / 2
+    size = (step.abs() * (D.abs() @ W.abs())).sum()
+    assert abs(float(slope - (dx.double() * step).sum())) <= (257 + blocks(V)) * 2.0 ** -24 * float(size)
+    # and the quantizing itself: half an e4m3 step of every d_l (2^-4 of it, or 2^-10 of its block's scale)
+    exact = dl.double() @ W
+    off = 2.0 ** -4 * dl.double().abs() + 2.0 ** -10 * ds.double()[:, at]
+    assert bool(((dx.double() - exact).abs() <= off @ W.abs() + (257 + blocks(V)) * 2.0 ** -24 * (D.abs() @ W.abs())).all())
