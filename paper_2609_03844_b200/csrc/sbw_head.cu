@@ -114,6 +114,12 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
                  "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(form), "r"(static_cast<uint32_t>(add)) : "memory");
 }
+// A load that stays where it is written: the compiler may move an ordinary one behind the wait that it is to overlap.
+__device__ __forceinline__ float load_now(const float *p) {
+    float v;
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -417,12 +423,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             Pair acc[PART / 2];
 #pragma unroll
             for (int i = 0; i < PART / 2; ++i) acc[i] = 0ull;
-            float sx = __ldg(xs), sw = __ldg(ws);        // a block's scales are on their way while the one before is added
+            float sx = load_now(xs), sw = load_now(ws);        // a block's scales are on their way while the one before is added
             for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
                 const float s = sx * sw;
                 if (kb + 1 < a.kblocks) {
-                    sx = __ldg(xs + kb + 1);
-                    sw = __ldg(ws + kb + 1);
+                    sx = load_now(xs + kb + 1);
+                    sw = load_now(ws + kb + 1);
                 }
                 greens.advance(a, staging, per_block, tile_col, warp - 4, lane);
                 if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up));
