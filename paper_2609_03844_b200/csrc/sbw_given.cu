@@ -351,37 +351,45 @@ struct Row {
         }
         return w;
     }
-    // f(vector, j) for the thread's vectors from global memory, biased
+    // f(vector, j) for the thread's vectors from global memory, biased.  Whole batches of whole vectors need no checks.
     template <typename F>
     __device__ __forceinline__ void each_loaded(F f) const {
-        for (uint32_t j0 = threadIdx.x; j0 < vectors; j0 += kInFlight * kGivenThreads) {
+        const uint32_t end = whole_from + wholes;
+        const uint4 *const from = reinterpret_cast<const uint4 *>(base) + vec0;
+        const uint32_t vg = a.vocab_offset + col0;
+        uint32_t j = whole_from + threadIdx.x;
+        for (; j + (kInFlight - 1) * kGivenThreads < end; j += kInFlight * kGivenThreads) {
             uint4 w[kInFlight];
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                const uint32_t j = j0 + u * kGivenThreads;
-                w[u] = whole(j) ? raw(j) : make_uint4(0u, 0u, 0u, 0u);
-            }
+            for (int u = 0; u < kInFlight; ++u) w[u] = __ldg(from + j + u * kGivenThreads);
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) {
-                const uint32_t j = j0 + u * kGivenThreads;
-                if (j >= vectors) break;
-                if (whole(j)) bias_vector<DTYPE, SCHEME>(w[u], rs, a.vocab_offset + col0 + j * VEC, a.bias);
-                else w[u] = ragged(j);
-                f(w[u], j);
+                bias_vector<DTYPE, SCHEME>(w[u], rs, vg + (j + u * kGivenThreads) * VEC, a.bias);
+                f(w[u], j + u * kGivenThreads);
             }
         }
+#pragma unroll 1
+        for (; j < end; j += kGivenThreads) {
+            uint4 w = __ldg(from + j);
+            bias_vector<DTYPE, SCHEME>(w, rs, vg + j * VEC, a.bias);
+            f(w, j);
+        }
+        // the row's ragged ends
+        if (threadIdx.x < 2u) {
+            const uint32_t at = threadIdx.x == 0u ? 0u : vectors - 1u;
+            if (vectors > threadIdx.x && !whole(at)) f(ragged(at), at);
+        }
     }
-    // f(vector, j) for the thread's vectors, biased and settled
+    // f(vector, j) for the thread's vectors, biased.  Not settled where they come from global memory: NaN and -0 have the
+    // weights that -inf and +0 have.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         if constexpr (RESIDENT) {
             for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(slice[j], j);
+        } else if (infinite) {
+            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(vector(j), j);
         } else {
-            each_loaded([&](uint4 w, uint32_t j) {
-                settle<DTYPE>(w);
-                if (infinite) only_infinite<DTYPE>(w);
-                f(w, j);
-            });
+            each_loaded(f);
         }
     }
     // One of them.
