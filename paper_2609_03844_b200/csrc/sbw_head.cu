@@ -331,9 +331,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const uint32_t tmem = tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // The epilogue's sums take more registers than an even share; the split is the launch's total (168 x 384).
+    // The sums of a 128 x 256 tile take more registers than an even share.  The split is the whole of what the launch has,
+    // which launch_head checks: a warpgroup waits for registers that are not there for good.
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if constexpr (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0 && lane == 0) {
             uint32_t stage = 0, parity = 0;
             int64_t issued = 0;
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         }
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        if constexpr (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         const int quarter = warp % 4, wg = warp / 4 - 1;
         uint32_t buf = 0, parity = 0;
         int64_t seeds_of = -1;                           // first row of the tile whose seeds are there
@@ -551,6 +552,9 @@ int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t
     const auto kernel = head_kernel<DTYPE, SCHEME, BN>;
     static std::atomic<uint64_t> prepared{0};
     if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
+        cudaFuncAttributes f;
+        SBW_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
+        if (BN == 256 && f.numRegs * kHeadThreads < 40 * 128 + 232 * 256) return SBW_ERR_UNSUPPORTED;
         SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynamicBytes));
         prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
