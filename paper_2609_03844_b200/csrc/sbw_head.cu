@@ -50,7 +50,7 @@ struct HeadArgs {
     uint32_t B, V, kblocks;
     uint32_t m_tiles;
     int64_t tiles;
-    uint32_t x_bytes;          // of one stage's block of hidden states
+    uint32_t x_bytes;          // of one stage's block of hidden states that are copied
     uint32_t stages;
     uint32_t strided;          // rows of the logits do not start on 8-byte boundaries
     const int32_t *ctx;
@@ -300,12 +300,22 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     volatile uint32_t *const gave_up = &gave_up_slot;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t stages_at = (smem_addr(dynamic_smem) + 1023u) & ~1023u;
-    const uint32_t stage_bytes = kWBytes + a.x_bytes;
+    const uint32_t stage_bytes = kWBytes + kTileM * kBlock, copied = kWBytes + a.x_bytes;
     uint32_t *const staging = reinterpret_cast<uint32_t *>(
         dynamic_smem + (stages_at - smem_addr(dynamic_smem)) + a.stages * stage_bytes);
     const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
     const uint32_t ready = empty + 8 * kMaxStages, taken = ready + 8 * NBUF, last = taken + 8 * NBUF;
 
+    // Rows of hidden states that are not there are 0 in every stage: the matrix unit multiplies 128 rows whatever B is, and
+    // other bytes in their place cost power and so clocks (B = 1, 128256 x 4096 back to back: 114 us with the next stage's
+    // bytes there and 11 stages, 109 with zeros and 6).
+    if (a.x_bytes < kTileM * kBlock) {
+        uint8_t *const all = dynamic_smem + (stages_at - smem_addr(dynamic_smem));
+        for (uint32_t s = 0; s < a.stages; ++s)
+            for (uint32_t i = a.x_bytes + threadIdx.x * 16; i < kTileM * kBlock; i += kHeadThreads * 16)
+                *reinterpret_cast<uint4 *>(all + s * stage_bytes + kWBytes + i) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kMaxStages; ++i) {
             barrier_init(full + 8 * i, 1);
@@ -331,10 +341,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const uint32_t tmem = tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // The sums of a 128 x 256 tile take more registers than an even share.  The split is the whole of what the launch has,
-    // which launch_head checks: a warpgroup waits for registers that are not there for good.
+    // The epilogue's warps take more registers than an even share (64 x 128256 x 4096 watermarked: 162 us without, 145 with
+    // it).  The split is the whole of what the launch has, which launch_head checks: a warpgroup would wait for good for
+    // registers that are not there.
     if (warp < 4) {
-        if constexpr (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0 && lane == 0) {
             uint32_t stage = 0, parity = 0;
             int64_t issued = 0;
@@ -345,7 +356,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     ok = barrier_wait(empty + 8 * stage, parity ^ 1u, gave_up);
                     if (!ok) break;
                     const uint32_t at = stages_at + stage * stage_bytes;
-                    barrier_expect(full + 8 * stage, stage_bytes);
+                    barrier_expect(full + 8 * stage, copied);
                     copy_block(at, &map_w, static_cast<int>(kb) * kBlock, v0, full + 8 * stage);
                     copy_block(at + kWBytes, &map_x, static_cast<int>(kb) * kBlock, m0, full + 8 * stage);
                     ++issued;
@@ -393,7 +404,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         }
         __syncwarp();
     } else {
-        if constexpr (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         const int quarter = warp % 4, wg = warp / 4 - 1;
         uint32_t buf = 0, parity = 0;
         int64_t seeds_of = -1;                           // first row of the tile whose seeds are there
@@ -535,10 +546,7 @@ int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t
     if (int rc = current_device_info(&di)) return rc;
     const int box_m = a.B < kTileM ? static_cast<int>((a.B + 7) / 8 * 8) : kTileM;
     a.x_bytes = static_cast<uint32_t>(box_m) * kBlock;
-    const uint32_t stage_bytes = BN * kBlock + a.x_bytes;
-    // the matrix unit reads 128 rows of hidden states whatever x_bytes is: behind the last stage lies the
-    // staging area, which is larger than what that takes
-    static_assert(kStagingBytes >= kTileM * kBlock, "");
+    const uint32_t stage_bytes = BN * kBlock + kTileM * kBlock;
     a.stages = (kMaxDynamicBytes - 1024 - kStagingBytes) / stage_bytes;
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     const size_t bytes = 1024 + a.stages * stage_bytes + kStagingBytes;
@@ -552,9 +560,11 @@ int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t
     const auto kernel = head_kernel<DTYPE, SCHEME, BN>;
     static std::atomic<uint64_t> prepared{0};
     if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
+#ifndef SBW_DEBUG   // separate compilation, as the bounds-flag build has it, leaves the split out
         cudaFuncAttributes f;
         SBW_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
-        if (BN == 256 && f.numRegs * kHeadThreads < 40 * 128 + 232 * 256) return SBW_ERR_UNSUPPORTED;
+        if (f.numRegs * kHeadThreads < 40 * 128 + 232 * 256) return SBW_ERR_UNSUPPORTED;
+#endif
         SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynamicBytes));
         prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
