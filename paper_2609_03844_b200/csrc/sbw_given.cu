@@ -8,17 +8,22 @@
 // question, asked up to three times per row: at which candidate does the running number (top-k) or the
 // running weight (top-p, then the draw) reach a target?
 //
-// A row is read from memory once.  A cluster of CTAs keeps its biased logits in shared memory, a slice
-// per CTA, and passes over them there:
-//   maximum    while loading
-//   histogram  1024 bins by the weight's exponent and six bits of its mantissa, down to 2^-16 of the
-//              maximum: the number of candidates and the sum of the other 17 bits (32-bit counters, native
-//              adds).  Weights below that are summed in registers.
-//   lists      the first CTA scans the bins, asks the others for the candidates of the first bins up to
-//              the one that is looked for (of that bin alone if those are too many for the list), sorts
-//              them and walks the running sums.  The first list usually answers all questions.
-// A bin too full for the list is split by the candidates' bits, 1024 ways at a time; candidates of equal
-// value, however many, are counted by column.
+// A row belongs to one CTA, or to a cluster of up to 8 where there are fewer rows than SMs.  Two ways of doing it:
+//   by value    (bf16) few values are distinct: one pass counts them, before the maximum is known; weights and all three
+//               questions are then a matter of the counters, and a second pass, from L2, finds the column.
+//   by weight   (fp32, and the rare bf16 rows that the counters do not hold)
+//     maximum    one pass
+//     histogram  1024 bins by the weight's exponent and six bits of its mantissa, down to 2^-16 of the maximum: the
+//                number of candidates and the sum of the other 17 bits (32-bit counters, native adds).  Weights below
+//                that are summed in registers.
+//     lists      the first CTA scans the bins, asks all for the candidates of the first bins up to the one that is looked
+//                for (of that bin alone if those are too many for the list), sorts them and walks the running sums.  The
+//                first list usually answers all questions.
+//     A bin too full for the list is split by the candidates' bits, 1024 ways at a time; candidates of equal value,
+//     however many, are counted by column.  Plain rows are read again by every pass; watermarked ones stay in the
+//     cluster's shared memory, since the hash costs more than a pass.
+// Bound (1024 x 128256): bf16 by the integer pipe and the adds to shared memory of the counting pass, 166 us where the bytes
+// take 40; fp32 by the three readings of rows that L2 does not hold, 420 us where the bytes take 80.
 #include <atomic>
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -48,7 +53,7 @@ constexpr int kCountingSort = 128;         // a list up to this length is sorted
 constexpr int kPrefixCap = 1024;           // a list from the first candidate on is made up to this length
 constexpr int kMaxParts = 8;
 constexpr int64_t kMaxGivenV = 320 * 1024;
-constexpr int64_t kSliceBytes = 68 * 1024;           // two CTAs with such a slice fit on an SM
+constexpr int64_t kSliceBytes = 68 * 1024;           // of a row in a CTA's shared memory, before more CTAs share it
 // A sum of 17 bits holds 32768 candidates: every other warp of a CTA has its own.  The tail's sums in
 // registers hold 128 weights of 25 bits.
 static_assert(kMaxGivenV / kMaxParts <= 61440 && kSliceBytes / 2 <= 61440, "");
@@ -1017,9 +1022,8 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
     cl.order(done);
 }
 
-// fp32 rows.  Plain ones are read again from L2 by every pass, a CTA per row if there are as many rows as SMs (256 x 151936:
-// 330 us with the row resident in the shared memory of a cluster, which then waits for its first CTA); watermarked ones are
-// resident, since the hash costs more than a pass.
+// fp32 rows.  Plain ones are read again by every pass, a CTA per row if there are as many rows as SMs (256 x 151936: 111 us;
+// 330 with the row resident in the shared memory of a cluster, which then waits for its first CTA).
 template <int DTYPE, int SCHEME>
 using RowOf = Row<DTYPE, SCHEME, SCHEME != kSchemeNone>;
 template <int DTYPE, int SCHEME>

@@ -2,7 +2,7 @@
 // in which sbw_head_logits takes hidden states (blocks of one row) and weights (blocks of 128 rows).
 //
 //     scale = max(amax / 448, 2^-126)       448 = the largest finite e4m3 value
-//     code  = e4m3(x / scale)               both divisions IEEE fp32, the code to nearest even
+//     code  = e4m3(x / scale)               both quotients correctly rounded fp32, the code to nearest even
 //
 // One pass: a block's elements stay in registers between the maximum and the division, so every
 // element is read once and every code written once.
