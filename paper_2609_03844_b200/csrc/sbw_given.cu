@@ -1371,27 +1371,55 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
 
 // ---- host -----------------------------------------------------------------------------------
 
+// A launch of clusters of `parts` CTAs.
 template <typename K>
-int launch_row_clusters(K kernel, const GivenArgs &a, int64_t B, size_t bytes, int most_bytes, std::atomic<uint64_t> &prepared,
-                        const DeviceInfo &di, cudaStream_t stream) {
-    if (B > 0x7fffffffLL / a.parts) return SBW_ERR_UNSUPPORTED;
-    if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
-        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_bytes));
-        prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(B * a.parts));
-    cfg.blockDim = dim3(kGivenThreads);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = stream;
+struct RowClusters {
+    K kernel;
+    size_t bytes;              // of shared memory per CTA
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.parts;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = a.parts > 1 ? 1 : 0;
-    SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+    cudaLaunchConfig_t config(int64_t rows, int64_t parts, cudaStream_t stream) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(rows * parts));
+        cfg.blockDim = dim3(kGivenThreads);
+        cfg.dynamicSmemBytes = bytes;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = parts > 1 ? 1 : 0;
+        return cfg;
+    }
+    int launch(const GivenArgs &a, int64_t B, cudaStream_t stream) {
+        if (B > 0x7fffffffLL / a.parts) return SBW_ERR_UNSUPPORTED;
+        const cudaLaunchConfig_t cfg = config(B, a.parts, stream);
+        SBW_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+        return SBW_OK;
+    }
+};
+
+// CTAs per row where any number will do: the most, up to 8, with which all rows are under way at once -- a second round
+// costs a row's fixed phases again (37 x 128256 bf16 watermarked: 72 us with 4 CTAs in two rounds, 53 in one with 2) -- as
+// long as each finds a vector per thread.  Clusters lie within a GPC, so how many fit is asked, once per device.
+template <typename K>
+int parts_in_one_round(RowClusters<K> &rows, int64_t B, int64_t row_vectors, int device, std::atomic<int> (&fit)[64][4], int64_t *parts) {
+    *parts = 1;
+    for (int i = 3; i > 0; --i) {
+        const int64_t p = int64_t(1) << i;
+        if (row_vectors <= p / 2 * kGivenThreads) continue;
+        int n = fit[device][i].load(std::memory_order_acquire);
+        if (n == 0) {
+            const cudaLaunchConfig_t cfg = rows.config(64, p, nullptr);
+            SBW_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, rows.kernel, &cfg));
+            if (n < 1) n = -1;
+            fit[device][i].store(n, std::memory_order_release);
+        }
+        if (B <= n) {
+            *parts = p;
+            break;
+        }
+    }
     return SBW_OK;
 }
 
@@ -1401,31 +1429,33 @@ int launch_given(GivenArgs &a, int64_t B, cudaStream_t stream) {
     if (int rc = current_device_info(&di)) return rc;
     if (di.device >= 64) return SBW_ERR_UNSUPPORTED;
     static std::atomic<uint64_t> prepared{0};
+    static std::atomic<int> fit[64][4];
     constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
+    constexpr bool kByValue = DTYPE == SBW_DTYPE_BF16, kResident = !kByValue && SCHEME != kSchemeNone;
+    using Shared = typename Row<DTYPE, SCHEME, kResident>::Shared;
+    constexpr size_t kWeights = (sizeof(Shared) + 15) / 16 * 16;
+    constexpr size_t kShared = kByValue && sizeof(CodesShared) > kWeights ? sizeof(CodesShared) : kWeights;
+    // the most that V, up to its limit, asks of a CTA
+    constexpr int64_t kLargest = (kMaxGivenV + 2 * VEC) / VEC * 16 / kMaxParts + 16;
+    constexpr int64_t kSlice = !kResident ? 0 : kLargest > kSliceBytes + 16 ? kLargest : kSliceBytes + 16;
     const int64_t row_vectors = (a.V + 2 * (VEC - 1)) / VEC;
-    int64_t parts = 1;
-    if constexpr (DTYPE == SBW_DTYPE_BF16 || SCHEME == kSchemeNone) {
-        // one CTA per row unless that leaves SMs without work
-        using Shared = typename Row<DTYPE, SCHEME, false>::Shared;
-        constexpr int kBytes = static_cast<int>(sizeof(Shared) > sizeof(CodesShared) ? sizeof(Shared) : sizeof(CodesShared));
-        while (parts < kMaxParts && B * parts <= di.sm_count && row_vectors > parts * kGivenThreads) parts *= 2;
-        a.parts = static_cast<uint32_t>(parts);
-        a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
-        if constexpr (DTYPE == SBW_DTYPE_BF16) return launch_row_clusters(given_codes_kernel<SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
-        else return launch_row_clusters(given_kernel<DTYPE, SCHEME>, a, B, kBytes, kBytes, prepared, di, stream);
-    } else {
-        // CTAs per row: as many as its slices need, and more where few rows would leave SMs without work
-        using Shared = typename RowOf<DTYPE, SCHEME>::Shared;
-        constexpr size_t kShared = (sizeof(Shared) + 15) / 16 * 16;
-        // the most that V, up to its limit, asks of a CTA
-        constexpr int64_t kLargest = (kMaxGivenV + 2 * VEC) / VEC * 16 / kMaxParts + 16;
-        constexpr int kMost = static_cast<int>(kShared + (kLargest > kSliceBytes + 16 ? kLargest : kSliceBytes + 16));
-        while (parts < kMaxParts && (row_vectors * 16 > parts * kSliceBytes || (B * parts * 2 <= di.sm_count && row_vectors > parts * kGivenThreads)))
-            parts *= 2;
-        a.parts = static_cast<uint32_t>(parts);
-        a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
-        return launch_row_clusters(given_kernel<DTYPE, SCHEME>, a, B, kShared + static_cast<size_t>(a.part_vectors) * 16, kMost, prepared, di, stream);
+    const auto kernel = [] {
+        if constexpr (kByValue) return given_codes_kernel<SCHEME>;
+        else return given_kernel<DTYPE, SCHEME>;
+    }();
+    if (!(prepared.load(std::memory_order_acquire) >> di.device & 1)) {
+        SBW_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared + kSlice)));
+        prepared.fetch_or(uint64_t(1) << di.device, std::memory_order_release);
     }
+    RowClusters<decltype(kernel)> rows = {kernel, kShared + kSlice, {}};
+    int64_t parts;
+    if (int rc = parts_in_one_round(rows, B, row_vectors, di.device, fit, &parts)) return rc;
+    if (kResident)
+        while (parts < kMaxParts && row_vectors * 16 > parts * kSliceBytes) parts *= 2;
+    a.parts = static_cast<uint32_t>(parts);
+    a.part_vectors = static_cast<uint32_t>((row_vectors + parts - 1) / parts);
+    rows.bytes = kShared + (kResident ? static_cast<size_t>(a.part_vectors) * 16 : 0);
+    return rows.launch(a, B, stream);
 }
 
 }  // namespace
