@@ -54,10 +54,9 @@ constexpr int kPrefixCap = 1024;           // a list from the first candidate on
 constexpr int kMaxParts = 8;
 constexpr int64_t kMaxGivenV = 320 * 1024;
 constexpr int64_t kSliceBytes = 68 * 1024;           // of a row in a CTA's shared memory, before more CTAs share it
-// A sum of 17 bits holds 32768 candidates: every other warp of a CTA has its own.  The tail's sums in
-// registers hold 128 weights of 25 bits.
-static_assert(kMaxGivenV / kMaxParts <= 61440 && kSliceBytes / 2 <= 61440, "");
-static_assert(kMaxGivenV / kMaxParts + 16 <= 120 * kGivenThreads && kSliceBytes / 2 <= 120 * kGivenThreads, "");
+// A sum of 17 bits holds 32768 candidates: of a resident part every other warp has its own, of a streamed row every warp.
+static_assert(kMaxGivenV / kMaxParts / 2 + 8 * kGivenThreads <= 32768 && kSliceBytes / 2 / 2 + 8 * kGivenThreads <= 32768, "");
+static_assert(kMaxGivenV / kGivenWarps + 8 * 32 + 16 <= 32768, "");
 constexpr uint32_t kLimb = 12;                       // of a split's two sums
 
 struct GivenArgs {
