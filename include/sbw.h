@@ -471,9 +471,9 @@ int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32
  * one fp32 scale for each block of 128 columns: the form in which sbw_head_logits takes its operands.
  * Over the elements of a block, amax the largest magnitude:
  *     scale = max(amax / 448, 2^-126)      code = e4m3(x / scale)
- * (both divisions in fp32, the code rounded to nearest even and held within +-448).  x is within half an
- * e4m3 step of code * scale.  A block that holds a NaN or an infinity has a scale that is not finite, and code times
- * scale is NaN throughout it.
+ * (both divisions in fp32 and correctly rounded, the code rounded to nearest even and held within +-448; a zero keeps
+ * its sign).  x is within half an e4m3 step of code * scale.  A block that holds a NaN or an infinity has a scale that
+ * is not finite, and code times scale is NaN throughout it.
  *   x           device, [R, ld] of `dtype`, R >= 0 rows, K > 0 columns, ld >= K; any alignment of an element
  *               (rows that start on 16-byte boundaries, and on 8-byte ones in `out`, take the vectorised path).
  *   block_rows  1: a scale per row and 128 columns (hidden states).  128: a scale per 128 x 128 block (weights).

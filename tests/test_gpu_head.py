@@ -226,3 +226,30 @@ def test_gradient_of_the_hidden_states():
     exact = dl.double() @ W
     off = 2.0 ** -4 * dl.double().abs() + 2.0 ** -10 * ds.double()[:, at]
     assert bool(((dx.double() - exact).abs() <= off @ W.abs() + (257 + blocks(V)) * 2.0 ** -24 * (D.abs() @ W.abs())).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantizer_keeps_the_sign_of_zero(block_rows, dtype):
+    """-0 / scale is -0, code 0x80, whatever the scale: ordinary ones, those of blocks whose quotients are divisions (scales from
+    2^90 on and below 2^-90), blocks of zeros alone; so is a negative quotient too small for a code."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    R, K = 130, 1300                                          # the last row and the last block are ragged
+    x = torch.zeros(R, K)
+    x[:, 1::2] = -0.0
+    for kb, top in enumerate((1.0, 3.0e4, 2.0 ** 100, 2.0 ** -100, 2.0 ** -80, 0.0, 448.0, 0.7, 2.0 ** 98, 2.0 ** -82, 5.0)):
+        x[:, kb * 128 + 3] = top
+        x[:, kb * 128 + 5] = -top * 2.0 ** -30
+        x[:, kb * 128 + 6] = top * 2.0 ** -30
+    x = x.to(dtype)
+    want = torch.where(torch.signbit(x), 0x80, 0).to(torch.uint8)
+    want[:, 3::128] = torch.where(x[:, 3::128] > 0, 0x7E, 0).to(torch.uint8)
+    for extra in (0, 1, 16):
+        src = torch.zeros((R, K + extra), dtype=dtype, device="cuda")
+        src[:, :K] = x.cuda()
+        out = torch.full((R, K + extra), 0x55, dtype=torch.uint8, device="cuda")
+        s = torch.empty(-(-R // block_rows), blocks(K), device="cuda")
+        sbw.sbw_quantize_fp8(src[:, :K], out.view(E4M3)[:, :K], s, block_rows=block_rows)
+        assert torch.equal(out[:, :K].cpu(), want)
