@@ -38,6 +38,7 @@ extern __device__ unsigned int g_sbw_debug[4];   // [0]: bit mask of failed site
 #define SBW_SITE_WEIGHT 11
 #define SBW_SITE_HEAD_STORE 12
 #define SBW_SITE_GIVEN_LOAD 13
+#define SBW_SITE_HEAD_COPY 14
 
 namespace sbw {
 

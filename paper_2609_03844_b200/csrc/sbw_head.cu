@@ -61,6 +61,9 @@ struct HeadArgs {
     int W;
     uint32_t vocab_offset;
     BiasParams bias;
+#ifdef SBW_DEBUG
+    int64_t stop_at;           // a CTA's products stop at this block, as where a wait ran out
+#endif
 };
 
 // ---- one-line PTX ---------------------------------------------------------------------------
@@ -343,6 +346,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
+    int64_t issued = 0;                                  // by thread 0: blocks copied
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // The epilogue's warps take more registers than an even share (64 x 128256 x 4096 watermarked: 162 us without, 145 with
@@ -352,7 +356,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0 && lane == 0) {
             uint32_t stage = 0, parity = 0;
-            int64_t issued = 0;
             bool ok = true;
             for (int64_t t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
                 const int m0 = static_cast<int>(t % a.m_tiles) * kTileM, v0 = static_cast<int>(t / a.m_tiles) * BN;
@@ -370,18 +373,28 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     }
                 }
             }
-            if (!ok) {       // copies in flight have to land before the CTA's shared memory goes
-                for (uint32_t i = 0; i < a.stages && issued > 0; ++i) {
-                    --issued;
-                    barrier_wait(full + 8 * static_cast<uint32_t>(issued % a.stages),
-                                 static_cast<uint32_t>(issued / a.stages) & 1u, nullptr);
-                }
+            // Copies in flight have to land before the CTA's shared memory goes.  Where the products stopped nobody else has
+            // waited for the last ones, whether this thread gave up or had issued everything by then.
+            for (uint32_t i = 0; i < a.stages && i < issued; ++i) {
+                const int64_t n = issued - 1 - i;
+                barrier_wait(full + 8 * static_cast<uint32_t>(n % a.stages), static_cast<uint32_t>(n / a.stages) & 1u, nullptr);
             }
         } else if (warp == 1 && lane == 0) {
             uint32_t stage = 0, parity = 0, buf = 0, buf_parity = 0;
             bool ok = true;
+#ifdef SBW_DEBUG
+            int64_t block = 0;
+#endif
             for (int64_t t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
                 for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
+#ifdef SBW_DEBUG
+                    if (block++ == a.stop_at) {
+                        for (const uint64_t start = now_ns(); now_ns() - start < 1000000ull;) {}      // products under way end first
+                        *gave_up = 1u;
+                        ok = false;
+                        break;
+                    }
+#endif
                     ok = barrier_wait(taken + 8 * buf, buf_parity ^ 1u, gave_up) &&
                          barrier_wait(full + 8 * stage, parity, gave_up);
                     if (!ok) break;
@@ -505,6 +518,12 @@ uint32_t r[2][16];
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+#ifdef SBW_DEBUG
+    if (threadIdx.x == 0)
+        for (int64_t n = issued - 1; n >= 0 && n >= issued - a.stages; --n)
+            (void)SBW_CHECKED(barrier_try(full + 8 * static_cast<uint32_t>(n % a.stages), static_cast<uint32_t>(n / a.stages) & 1u),
+                              SBW_SITE_HEAD_COPY);
+#endif
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
@@ -512,6 +531,10 @@ uint32_t r[2][16];
 }
 
 // ---- host -----------------------------------------------------------------------------------
+
+#ifdef SBW_DEBUG
+std::atomic<int64_t> debug_stop_at{-1};
+#endif
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -640,6 +663,9 @@ extern "C" int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scale
     a.bias.delta = in_precision;
     a.bias.delta_bf16 = dtype == SBW_DTYPE_BF16 ? static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(delta))) : 0u;
     a.bias.weyl = make_weyl();
+#ifdef SBW_DEBUG
+    a.stop_at = debug_stop_at.load();
+#endif
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (dtype == SBW_DTYPE_F32) {
         if (!marked) return launch_head<SBW_DTYPE_F32, kSchemeNone>(a, x, ld_x, w, ld_w, K, s);
@@ -650,3 +676,12 @@ extern "C" int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scale
     return scheme == SBW_SCHEME_CONTEXT ? launch_head<SBW_DTYPE_BF16, SBW_SCHEME_CONTEXT>(a, x, ld_x, w, ld_w, K, s)
                                         : launch_head<SBW_DTYPE_BF16, SBW_SCHEME_SELFSALT>(a, x, ld_x, w, ld_w, K, s);
 }
+
+#ifdef SBW_DEBUG
+// Bounds-flag build only: from the next call on, every CTA's products stop at its block number `block` (counted over its tiles),
+// as they do where a wait ran out; below 0 they do not.
+extern "C" int sbw_debug_head_stop(int64_t block) {
+    sbw::debug_stop_at.store(block);
+    return SBW_OK;
+}
+#endif
