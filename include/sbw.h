@@ -500,8 +500,17 @@ int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32
  * An e4m3 NaN or a scale that is not finite makes the logits that it enters NaN or infinite.  Equal calls give
  * equal bits; a row's logits do not depend on the other rows.  The gradient of the hidden states is the same product
  * with the transposed weights (codes and scales both transposed; blocks of 128 x 128 stay blocks):
- * d_x = d_l w, with d_l quantized in blocks of one row.
+ * d_x = d_l w, with d_l quantized in blocks of one row.  The caller makes and keeps the transposed copy.
+ * A product of two scales beyond fp32's range is infinite or 0, as fp32 has it.
  * No workspace; calls on different streams may overlap.
+ * The kernel hands tiles on inside each CTA.  A wait there that does not end within two seconds of running (which no
+ * call is known to reach) gives up: the call still ends, the rest of that CTA's logits are NaN, and sbw_head_gave_up
+ * counts the CTA.
+ *
+ * sbw_head_gave_up -- the number of CTAs in which such a wait gave up, on the current device since the library was
+ * loaded: a number that grew over a call means that its logits are not whole.  (sbw_sample_given takes NaN as
+ * -inf, so that it would draw from what is left.)
+ *   out_ctas    host.  Waits for the work before it in `stream`; SBW_ERR_UNSUPPORTED while `stream` is captured.
  */
 int sbw_quantize_fp8(const void *x, int dtype, int64_t R, int64_t K, int64_t ld, int64_t block_rows, void *out,
                      int64_t ld_out, float *scales, int64_t ld_scales, void *stream);
@@ -509,6 +518,7 @@ int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scales, int64_t 
                     int64_t ld_w, const float *w_scales, int64_t ld_w_scales, int64_t B, int64_t V, int64_t K,
                     void *logits, int dtype, int64_t ld, int64_t vocab_offset, const int32_t *ctx_tokens,
                     int ctx_width, uint64_t key, double gamma, float delta, int scheme, void *stream);
+int sbw_head_gave_up(uint64_t *out_ctas, void *stream);
 
 /*
  * sbw_sample_given -- one token per row from a random number that the caller gives, with temperature, top-k, top-p

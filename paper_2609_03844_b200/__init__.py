@@ -12,7 +12,7 @@ from .binding import (DTYPE_BF16, DTYPE_F32, SCHEME_CONTEXT, SCHEME_SELFSALT, Sb
                       sbw_sample_filtered_workspace_bytes,
                       sbw_detect_workspace_bytes, sbw_int_probe, sbw_sample_workspace_bytes,
                       sbw_token_logprobs, sbw_token_logprobs_backward, sbw_detect_weighted,
-                      sbw_quantize_fp8, sbw_head_logits, sbw_sample_given,
+                      sbw_quantize_fp8, sbw_head_logits, sbw_head_gave_up, sbw_sample_given,
                       MAX_TOP_LOGPROBS, sbw_version)
 
 __all__ = ["DTYPE_BF16", "DTYPE_F32", "SCHEME_CONTEXT", "SCHEME_SELFSALT", "SbwError", "lib",
@@ -24,5 +24,5 @@ __all__ = ["DTYPE_BF16", "DTYPE_F32", "SCHEME_CONTEXT", "SCHEME_SELFSALT", "SbwE
            "sbw_sample_filtered_workspace_bytes",
            "sbw_detect_workspace_bytes", "sbw_int_probe", "sbw_sample_workspace_bytes",
            "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted",
-           "sbw_quantize_fp8", "sbw_head_logits", "sbw_sample_given", "MAX_TOP_LOGPROBS",
+           "sbw_quantize_fp8", "sbw_head_logits", "sbw_head_gave_up", "sbw_sample_given", "MAX_TOP_LOGPROBS",
            "sbw_version"]

@@ -36,7 +36,7 @@ EXPORTS = ("sbw_version", "sbw_last_cuda_error", "sbw_bias_logits",
            "sbw_roc_auc_workspace_bytes", "sbw_roc_auc", "sbw_sample_filtered_workspace_bytes",
            "sbw_bias_sample_filtered", "sbw_roc_auc_batched", "sbw_bias_sample_shard_ids",
            "sbw_token_logprobs", "sbw_token_logprobs_backward", "sbw_detect_weighted", "sbw_quantize_fp8",
-           "sbw_head_logits", "sbw_sample_given")
+           "sbw_head_logits", "sbw_head_gave_up", "sbw_sample_given")
 
 _lib = None
 
@@ -154,6 +154,8 @@ def lib() -> ctypes.CDLL:
         L.sbw_head_logits.restype = i32
         L.sbw_head_logits.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, i64, vp, i32, u64,
                                       c.c_double, c.c_float, i32, vp]
+        L.sbw_head_gave_up.restype = i32
+        L.sbw_head_gave_up.argtypes = [vp, vp]
         L.sbw_sample_given.restype = i32
         L.sbw_sample_given.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32, u64, c.c_double, c.c_float, i32, vp, vp, vp, vp,
                                        vp, vp, vp, vp, vp]
@@ -701,6 +703,15 @@ def sbw_head_logits(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_
     _launch("sbw_head_logits", dev, stream, *given, B, V, K, logits.data_ptr(), _dtype_code(logits), ld, vocab_offset, ctx,
             W, key, gamma, delta, scheme)
     return logits
+
+
+def sbw_head_gave_up(device: int | None = None, stream=None) -> int:
+    """How many CTAs of :func:`sbw_head_logits` gave up a wait on ``device`` (default: the current one) since the library was
+    loaded.  0 unless something is wrong: a number that grew over a call means that some of its logits are NaN in place of
+    their values.  Waits for the work before it in ``stream``."""
+    out = ctypes.c_uint64()
+    _launch("sbw_head_gave_up", _current_device() if device is None else device, stream, ctypes.byref(out))
+    return out.value
 
 
 def sbw_sample_given(logits: torch.Tensor, uniforms: torch.Tensor, out_tokens: torch.Tensor, *, temperature: torch.Tensor,

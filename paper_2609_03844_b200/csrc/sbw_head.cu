@@ -20,8 +20,8 @@
 // 1000 W cap, 109); above, the fp32 sums of the epilogue's warps beside the products (2048 x 128256 x 4096: 1.08 ms in short
 // runs, 1.28 under the cap; the products alone take 0.65, with the copies 0.77).
 //
-// Every wait is bounded: one that does not end within kWaitLimit gives up, the rest of the CTA's logits
-// are NaN, and the kernel returns.
+// Every wait is bounded: one that does not end within kWaitLimit gives up, the rest of the CTA's logits are NaN, the kernel
+// returns, and sbw_head_gave_up tells of it.
 #include <atomic>
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -40,6 +40,7 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kMaxStages = 16;
 constexpr int kTmemColumns = 512;
 constexpr uint64_t kWaitLimit = 2000000000ull;      // nanoseconds
+constexpr uint64_t kLongestLook = 10000000ull;      // more than that between two looks at the clock is time switched out
 constexpr int kRowWords = 64;                        // of a row that go through the staging area at a time
 constexpr int kRowStride = kRowWords + 2;            // 8-byte accesses by row and by column without bank conflicts; the
                                                      // two words behind a row hold its watermark seed
@@ -63,8 +64,18 @@ struct HeadArgs {
     BiasParams bias;
 #ifdef SBW_DEBUG
     int64_t stop_at;           // a CTA's products stop at this block, as where a wait ran out
+    int64_t withhold_from;     // a CTA's blocks from this one on are not copied, so that the wait for them runs out
+    uint64_t wait_limit;
 #endif
 };
+
+__device__ unsigned long long g_gave_up;   // CTAs in which a wait gave up, since the module was loaded
+
+#ifdef SBW_DEBUG
+__device__ __forceinline__ uint64_t wait_limit(const HeadArgs &a) { return a.wait_limit; }
+#else
+__device__ __forceinline__ uint64_t wait_limit(const HeadArgs &) { return kWaitLimit; }
+#endif
 
 // ---- one-line PTX ---------------------------------------------------------------------------
 
@@ -93,15 +104,18 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
 }
 // Waits for the phase of the given parity to end; false if it did not within the limit or, where
 // `gave_up` is given, another thread of the CTA gave up.
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up) {
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up, uint64_t limit = kWaitLimit) {
     if (barrier_try(bar, parity)) return true;
-    const uint64_t start = now_ns();
+    uint64_t waited = 0, before = now_ns();
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 16; ++i)
             if (barrier_try(bar, parity)) return true;
         if (gave_up && *gave_up) return false;
-        if (now_ns() - start > kWaitLimit) {
+        const uint64_t now = now_ns();
+        waited += min(now - before, kLongestLook);
+        before = now;
+        if (waited > limit) {
             if (gave_up) *gave_up = 1u;
             return false;
         }
@@ -347,6 +361,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
     int64_t issued = 0;                                  // by thread 0: blocks copied
+    const uint64_t limit = wait_limit(a);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // The epilogue's warps take more registers than an even share (64 x 128256 x 4096 watermarked: 162 us without, 145 with
@@ -360,7 +375,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             for (int64_t t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
                 const int m0 = static_cast<int>(t % a.m_tiles) * kTileM, v0 = static_cast<int>(t / a.m_tiles) * BN;
                 for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
-                    ok = barrier_wait(empty + 8 * stage, parity ^ 1u, gave_up);
+#ifdef SBW_DEBUG
+                    if (issued == a.withhold_from) {
+                        ok = false;
+                        break;
+                    }
+#endif
+                    ok = barrier_wait(empty + 8 * stage, parity ^ 1u, gave_up, limit);
                     if (!ok) break;
                     const uint32_t at = stages_at + stage * stage_bytes;
                     barrier_expect(full + 8 * stage, copied);
@@ -377,7 +398,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             // waited for the last ones, whether this thread gave up or had issued everything by then.
             for (uint32_t i = 0; i < a.stages && i < issued; ++i) {
                 const int64_t n = issued - 1 - i;
-                barrier_wait(full + 8 * static_cast<uint32_t>(n % a.stages), static_cast<uint32_t>(n / a.stages) & 1u, nullptr);
+                if (!barrier_wait(full + 8 * static_cast<uint32_t>(n % a.stages), static_cast<uint32_t>(n / a.stages) & 1u, nullptr))
+                    *gave_up = 1u;
             }
         } else if (warp == 1 && lane == 0) {
             uint32_t stage = 0, parity = 0, buf = 0, buf_parity = 0;
@@ -395,8 +417,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                         break;
                     }
 #endif
-                    ok = barrier_wait(taken + 8 * buf, buf_parity ^ 1u, gave_up) &&
-                         barrier_wait(full + 8 * stage, parity, gave_up);
+                    ok = barrier_wait(taken + 8 * buf, buf_parity ^ 1u, gave_up, limit) &&
+                         barrier_wait(full + 8 * stage, parity, gave_up, limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t at = stages_at + stage * stage_bytes;
@@ -417,7 +439,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 }
             }
             commit(last);                              // no product is in flight when the tensor memory goes
-            barrier_wait(last, 0u, nullptr);
+            if (!barrier_wait(last, 0u, nullptr)) *gave_up = 1u;
         }
         __syncwarp();
     } else {
@@ -460,7 +482,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                     sw = load_now(ws + kb + 1);
                 }
                 greens.advance(a, staging, per_block, tile_col, warp - 4, lane);
-                if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up));
+                if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up, limit));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + wg * PART;
@@ -518,6 +540,7 @@ uint32_t r[2][16];
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (threadIdx.x == 0 && *gave_up) atomicAdd(&g_gave_up, 1ull);
 #ifdef SBW_DEBUG
     if (threadIdx.x == 0)
         for (int64_t n = issued - 1; n >= 0 && n >= issued - a.stages; --n)
@@ -533,7 +556,8 @@ uint32_t r[2][16];
 // ---- host -----------------------------------------------------------------------------------
 
 #ifdef SBW_DEBUG
-std::atomic<int64_t> debug_stop_at{-1};
+std::atomic<int64_t> debug_stop_at{-1}, debug_withhold_from{-1};
+std::atomic<uint64_t> debug_wait_limit{kWaitLimit};
 #endif
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -665,6 +689,8 @@ extern "C" int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scale
     a.bias.weyl = make_weyl();
 #ifdef SBW_DEBUG
     a.stop_at = debug_stop_at.load();
+    a.withhold_from = debug_withhold_from.load();
+    a.wait_limit = debug_wait_limit.load();
 #endif
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (dtype == SBW_DTYPE_F32) {
@@ -677,7 +703,29 @@ extern "C" int sbw_head_logits(const void *x, int64_t ld_x, const float *x_scale
                                         : launch_head<SBW_DTYPE_BF16, SBW_SCHEME_SELFSALT>(a, x, ld_x, w, ld_w, K, s);
 }
 
+extern "C" int sbw_head_gave_up(uint64_t *out_ctas, void *stream) {
+    using namespace sbw;
+    if (!out_ctas) return SBW_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus capture;
+    SBW_CUDA_TRY(cudaStreamIsCapturing(s, &capture));
+    if (capture != cudaStreamCaptureStatusNone) return SBW_ERR_UNSUPPORTED;
+    unsigned long long ctas = 0;
+    SBW_CUDA_TRY(cudaMemcpyFromSymbolAsync(&ctas, g_gave_up, sizeof(ctas), 0, cudaMemcpyDeviceToHost, s));
+    SBW_CUDA_TRY(cudaStreamSynchronize(s));
+    *out_ctas = ctas;
+    return SBW_OK;
+}
+
 #ifdef SBW_DEBUG
+// Bounds-flag build only: from the next call on, waits inside a CTA give up after limit_ns, and blocks from number
+// `withhold_from` of every CTA on (below 0: none) are not copied, so that the wait for them runs out.
+extern "C" int sbw_debug_head_waits(uint64_t limit_ns, int64_t withhold_from) {
+    sbw::debug_wait_limit.store(limit_ns);
+    sbw::debug_withhold_from.store(withhold_from);
+    return SBW_OK;
+}
+
 // Bounds-flag build only: from the next call on, every CTA's products stop at its block number `block` (counted over its tiles),
 // as they do where a wait ran out; below 0 they do not.
 extern "C" int sbw_debug_head_stop(int64_t block) {

@@ -122,3 +122,8 @@ def test_the_samplers_filters_keep_what_the_filtered_sampler_keeps(oracle, K, to
     kept = ref["kept"] if isinstance(ref, dict) else ref[1]
     p = np.full(B, np.float64(np.float32(top_p)) if top_p < 1 else 1.0)
     assert np.array_equal(given.sample(x, np.full(B, 0.5), np.full(B, tau), np.full(B, K), p)[2], kept)
+
+
+def test_a_place_for_the_number_of_waits_is_needed():
+    assert sbw.lib().sbw_head_gave_up(None, None) == INV
+    assert callable(sbw.sbw_head_gave_up) and "sbw_head_gave_up" in binding.EXPORTS and "sbw_head_gave_up" in sbw.__all__

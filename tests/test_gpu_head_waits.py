@@ -62,3 +62,48 @@ def test_copies_land_where_the_products_stop(dbg, B, K, tiles, stop, delta):  # 
     finally:
         dbg.sbw_debug_head_stop(-1)
     assert torch.equal(case.run(), case.want)
+
+
+LIMIT = 100_000_000                                       # ns
+
+
+def gave_up(dbg):  # noqa: F811
+    out = ctypes.c_uint64()
+    assert dbg.sbw_head_gave_up(ctypes.byref(out), None) == 0
+    return out.value
+
+
+@pytest.mark.parametrize("delta", [0.0, 2.0])
+@pytest.mark.parametrize("B,K,tiles,withheld", [(1, 128, 1, 0), (40, 512, 2, 5), (128, 256, 3, 2), (2, 1024, 2, 8)])
+def test_a_wait_that_runs_out_is_told(dbg, B, K, tiles, withheld, delta):  # noqa: F811
+    """A copy that never comes: the wait for it ends at its limit, every CTA is counted once, the context stays usable."""
+    require_gpu()
+    case = Case(dbg, B, K, tiles, delta)
+    dbg.sbw_debug_head_waits.argtypes = [ctypes.c_uint64, ctypes.c_int64]
+    dbg.sbw_head_gave_up.argtypes = sbw.lib().sbw_head_gave_up.argtypes
+    before = gave_up(dbg)
+    assert dbg.sbw_debug_head_waits(LIMIT, withheld) == 0
+    try:
+        case.check(withheld // blocks(K))
+    finally:
+        dbg.sbw_debug_head_waits(2_000_000_000, -1)
+    assert gave_up(dbg) == before + case.ctas
+    assert torch.equal(case.run(), case.want) and gave_up(dbg) == before + case.ctas
+
+
+def test_nothing_gave_up_in_the_release_build():
+    require_gpu()
+    x, w, xs, ws = codes(130, 300, 1), codes(700, 300, 2), scales(130, 300, 3), scales(blocks(700), 300, 4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    sbw.sbw_head_logits(x, xs, w, ws, torch.empty(130, 700, device="cuda"), stream=s)
+    assert sbw.sbw_head_gave_up(stream=s) == 0 and sbw.sbw_head_gave_up(0) == 0
+    graph = torch.cuda.CUDAGraph()
+    y = torch.zeros(1, device="cuda")
+    with torch.cuda.graph(graph):
+        y += 1
+        with pytest.raises(sbw.SbwError, match="UNSUPPORTED"):
+            sbw.sbw_head_gave_up()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(y) == 1.0
