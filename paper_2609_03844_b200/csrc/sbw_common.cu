@@ -62,6 +62,10 @@ __global__ void debug_selftest_kernel(int n) {
     (void)SBW_CHECKED(n < 0, 31);
 }
 }  // namespace
+// Bounds-flag build only: the check of an address, for a test of it on the host.
+extern "C" int sbw_debug_lies_in_rows(int64_t p, int64_t n, int64_t base, int size, int64_t rows, int64_t cols, int64_t ld) {
+    return sbw::lies_in_rows(reinterpret_cast<const void *>(p), n, reinterpret_cast<const void *>(base), size, rows, cols, ld);
+}
 extern "C" int sbw_debug_selftest(void *stream) {
     debug_selftest_kernel<<<1, 1, 0, static_cast<cudaStream_t>(stream)>>>(1);
     SBW_CUDA_TRY(cudaGetLastError());

@@ -11,7 +11,9 @@
 // Bounds-flag build (-DSBW_DEBUG, relocatable device code): the accesses of the bias, sampling and
 // detection kernels to rows, tokens and workspace, and every logit, gradient element and weight that
 // the log-probability, gradient and weighted kernels touch, are preceded by a check of their row /
-// column / position against the call's sizes.  A failed check records its site in a device-side
+// column / position against the call's sizes; those of the projection, the quantiser and the sampler from given
+// numbers to logits, values, codes, scales, settings and outputs by one of their address, and those to lists, bins
+// and resident rows in shared memory by one of their place.  A failed check records its site in a device-side
 // flag word; where the check's value is used the access is skipped too -- no trap, no device
 // assert -- and sbw_debug_flags() reads the words back.  It stands in for a memory checker on
 // machines where none can be run; release builds compile the checks away.
@@ -39,6 +41,12 @@ extern __device__ unsigned int g_sbw_debug[4];   // [0]: bit mask of failed site
 #define SBW_SITE_HEAD_STORE 12
 #define SBW_SITE_GIVEN_LOAD 13
 #define SBW_SITE_HEAD_COPY 14
+#define SBW_SITE_HEAD_LOAD 15
+#define SBW_SITE_GIVEN_SHARED 16
+#define SBW_SITE_GIVEN_OUTPUT 17
+#define SBW_SITE_QUANT_LOAD 18
+#define SBW_SITE_QUANT_STORE 19
+#define SBW_SITE_HEAD_SHARED 20
 
 namespace sbw {
 
@@ -55,6 +63,23 @@ inline int cuda_fail(cudaError_t e) {
         cudaError_t sbw_e_ = (expr);                        \
         if (sbw_e_ != cudaSuccess) return ::sbw::cuda_fail(sbw_e_); \
     } while (0)
+
+// For the checks: whether n elements of `size` bytes from p on lie in one row of a [rows, cols] matrix at base whose rows are
+// ld elements apart.  Found from the address alone, whatever the loops around an access take for granted.
+__host__ __device__ inline bool lies_in_rows(const void *p, int64_t n, const void *base, int size, int64_t rows, int64_t cols, int64_t ld) {
+    const int64_t off = static_cast<const char *>(p) - static_cast<const char *>(base);
+    if (off < 0 || off % size != 0) return false;
+    return off / size / ld < rows && off / size % ld + n <= cols;
+}
+#ifdef __CUDACC__
+// And whether `bytes` from p on lie in the CTA's dynamic shared memory, which begins at base.
+__device__ inline bool lies_in_shared(const void *p, uint32_t bytes, const void *base) {
+    uint32_t size;
+    asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(size));
+    const int64_t at = static_cast<const char *>(p) - static_cast<const char *>(base);
+    return at >= 0 && at + bytes <= size;
+}
+#endif
 
 struct DeviceInfo {
     int device;

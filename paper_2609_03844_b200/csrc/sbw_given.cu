@@ -61,7 +61,7 @@ constexpr uint32_t kLimb = 12;                       // of a split's two sums
 
 struct GivenArgs {
     const void *logits;
-    int64_t V, ld;
+    int64_t B, V, ld;
     uint32_t vocab_offset;
     const int32_t *ctx;
     int W;
@@ -101,6 +101,10 @@ struct Settings {
     uint32_t u32;
     Settings() = default;
     __device__ __forceinline__ Settings(const GivenArgs &a, int64_t row) {
+        if (!SBW_CHECKED(row >= 0 && row < a.B, SBW_SITE_GIVEN_LOAD)) {
+            *this = Settings{};
+            return;
+        }
         const float tau = a.temperature[row];
         const bool greedy = !(tau >= 1e-6f);
         c = greedy ? 1.0f : static_cast<float>(1.4426950408889634 / static_cast<double>(tau));
@@ -302,6 +306,12 @@ __device__ __forceinline__ void only_infinite(uint4 &w) {
     }
 }
 
+// Where a CTA's dynamic shared memory begins.
+[[maybe_unused]] __device__ __forceinline__ const void *room_base() {
+    extern __shared__ __align__(16) uint8_t given_smem[];
+    return given_smem;
+}
+
 // A CTA's part of a row.  Resident: its biased vectors are in shared memory after load().  Otherwise every pass reads
 // them from global memory (the second time from L2) and biases them anew.
 template <int DTYPE_, int SCHEME_, bool RESIDENT_>
@@ -339,7 +349,20 @@ struct Row {
         rs.init(a.bias.key, a.ctx + row * a.W, a.W);
     }
     __device__ __forceinline__ bool whole(uint32_t j) const { return j - whole_from < wholes; }
-    __device__ __forceinline__ uint4 raw(uint32_t j) const { return __ldg(reinterpret_cast<const uint4 *>(base) + vec0 + j); }
+    __device__ __forceinline__ bool lies_here(const void *p, int n) const { return lies_in_rows(p, n, a.logits, 16 / VEC, a.B, a.V, a.ld); }
+    __device__ __forceinline__ uint4 fetch(const uint4 *p) const {
+        if (!SBW_CHECKED(lies_here(p, VEC), SBW_SITE_GIVEN_LOAD)) return make_uint4(0u, 0u, 0u, 0u);
+        return __ldg(p);
+    }
+    __device__ __forceinline__ uint4 raw(uint32_t j) const { return fetch(reinterpret_cast<const uint4 *>(base) + vec0 + j); }
+    // Vector j of a resident part.
+    __device__ __forceinline__ uint4 kept(uint32_t j) const {
+        if (!SBW_CHECKED(lies_in_shared(slice + j, 16, room_base()), SBW_SITE_GIVEN_SHARED)) return make_uint4(0u, 0u, 0u, 0u);
+        return slice[j];
+    }
+    __device__ __forceinline__ void keep(uint32_t j, const uint4 &w) const {
+        if (SBW_CHECKED(lies_in_shared(slice + j, 16, room_base()), SBW_SITE_GIVEN_SHARED)) slice[j] = w;
+    }
     // The vector at an end of the row: what lies outside reads as -inf.  Biased.
     __device__ __forceinline__ uint4 ragged(uint32_t j) const {
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
@@ -348,7 +371,7 @@ struct Row {
 #pragma unroll 1
         for (int i = 0; i < VEC; ++i) {
             float x = -INFINITY;
-            if (SBW_CHECKED(j < vectors, SBW_SITE_GIVEN_LOAD) && col + i < static_cast<uint32_t>(a.V))
+            if (col + i < static_cast<uint32_t>(a.V) && SBW_CHECKED(lies_here(row_ptr + static_cast<int64_t>(col + i) * (16 / VEC), 1), SBW_SITE_GIVEN_LOAD))
                 x = biased_at<DTYPE, SCHEME>(row_ptr, col + i, rs, a.vocab_offset + col + i, a.bias);
             if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = __float_as_uint(x);
             else e[i >> 1] |= (i & 1) ? (__float_as_uint(x) & 0xffff0000u) : (__float_as_uint(x) >> 16);
@@ -365,7 +388,7 @@ struct Row {
         for (; j + (kInFlight - 1) * kGivenThreads < end; j += kInFlight * kGivenThreads) {
             uint4 w[kInFlight];
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) w[u] = __ldg(from + j + u * kGivenThreads);
+            for (int u = 0; u < kInFlight; ++u) w[u] = fetch(from + j + u * kGivenThreads);
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) {
                 bias_vector<DTYPE, SCHEME>(w[u], rs, vg + (j + u * kGivenThreads) * VEC, a.bias);
@@ -374,7 +397,7 @@ struct Row {
         }
 #pragma unroll 1
         for (; j < end; j += kGivenThreads) {
-            uint4 w = __ldg(from + j);
+            uint4 w = fetch(from + j);
             bias_vector<DTYPE, SCHEME>(w, rs, vg + j * VEC, a.bias);
             f(w, j);
         }
@@ -389,7 +412,7 @@ struct Row {
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         if constexpr (RESIDENT) {
-            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(slice[j], j);
+            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(kept(j), j);
         } else if (infinite) {
             for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) f(vector(j), j);
         } else {
@@ -398,7 +421,7 @@ struct Row {
     }
     // One of them.
     __device__ __forceinline__ uint4 vector(uint32_t j) const {
-        if constexpr (RESIDENT) return slice[j];
+        if constexpr (RESIDENT) return kept(j);
         uint4 w;
         if (whole(j)) {
             w = raw(j);
@@ -414,10 +437,12 @@ struct Row {
     __device__ __forceinline__ float value_at(uint32_t j, int i) const {
         float x;
         if constexpr (RESIDENT) {
+            if (!SBW_CHECKED(lies_in_shared(slice + j, 16, room_base()), SBW_SITE_GIVEN_SHARED)) return -INFINITY;
             x = DTYPE == SBW_DTYPE_F32 ? reinterpret_cast<const float *>(slice + j)[i]
                                        : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(slice + j)[i]);
         } else {
             const uint32_t col = col0 + j * VEC + i;
+            if (!SBW_CHECKED(lies_here(row_ptr + static_cast<int64_t>(col) * (16 / VEC), 1), SBW_SITE_GIVEN_LOAD)) return -INFINITY;
             x = fmaxf(biased_at<DTYPE, SCHEME>(row_ptr, col, rs, a.vocab_offset + col, a.bias) + 0.0f, -INFINITY);
             if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
         }
@@ -428,7 +453,7 @@ struct Row {
         float best = -INFINITY;
         each_loaded([&](uint4 w, uint32_t j) {
             settle<DTYPE>(w);
-            if constexpr (RESIDENT) slice[j] = w;
+            if constexpr (RESIDENT) keep(j, w);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) best = fmaxf(best, value(w, i));
         });
@@ -437,7 +462,11 @@ struct Row {
     __device__ __forceinline__ void keep_infinite() {
         infinite = true;
         if constexpr (RESIDENT)
-            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) only_infinite<DTYPE>(slice[j]);
+            for (uint32_t j = threadIdx.x; j < vectors; j += kGivenThreads) {
+                uint4 w = kept(j);
+                only_infinite<DTYPE>(w);
+                keep(j, w);
+            }
     }
     static __device__ __forceinline__ float value(const uint4 &w, int i) {
         const uint32_t *e = reinterpret_cast<const uint32_t *>(&w);
@@ -513,8 +542,9 @@ class Cluster {
                 float yy[2];
                 of_pair(y[i / 2], yy[0], yy[1]);
                 const bool real = yy[i & 1] >= rw.lowest;
-                const uint32_t u = real ? v[i] : 0u;
+                uint32_t u = real ? v[i] : 0u;
                 number += real;
+                if (!SBW_CHECKED(u < (kFirstBits << kLowBits) || (u >> kLowBits) - kFirstBits < kBins, SBW_SITE_GIVEN_SHARED)) u = 0u;
                 weigh_one(u, at_n + 4u * (u >> kLowBits), at_low + 4u * (u >> kLowBits), __float2uint_rz(__uint_as_float(u)), some);
             }
             tail += some;
@@ -601,6 +631,7 @@ class Cluster {
             }
             each_named(c, [&](uint32_t col, uint32_t, uint32_t dist) {
                 const uint32_t i = atomicAdd(&sh.list_n, 1u);
+                (void)SBW_CHECKED(i < kListCap, SBW_SITE_GIVEN_SHARED);      // a list is asked for where it holds all
                 if (i < kListCap) sh.list[i] = static_cast<unsigned long long>(dist) << 32 | col;
             });
             if (part != 0) {
@@ -612,7 +643,7 @@ class Cluster {
                 const uint32_t first = sh.list_at;
                 unsigned long long *const list = at(sh.list, 0);
                 for (uint32_t i = threadIdx.x; i < n; i += kGivenThreads)
-                    if (first + i < kListCap) list[first + i] = sh.list[i];
+                    if (SBW_CHECKED(first + i < kListCap, SBW_SITE_GIVEN_SHARED) && first + i < kListCap) list[first + i] = sh.list[i];
             }
         } else if (c.op == kSplit) {
             if (part != 0) {                             // the first CTA has cleared its own
@@ -621,6 +652,7 @@ class Cluster {
             }
             each_named(c, [&](uint32_t, uint32_t v, uint32_t dist) {
                 const uint32_t bin = (dist - c.dist_lo) >> c.shift;
+                if (!SBW_CHECKED(bin < kFine, SBW_SITE_GIVEN_SHARED)) return;
                 // of a bin the mantissa (the exponent is the bin's), of the tail the weight itself
                 const uint32_t q = c.bin_lo == kTail ? static_cast<uint32_t>(weight_of(v)) : (v & 0x7fffffu) | 0x800000u;
                 atomicAdd(&sh.fine.n[bin], 1u);
@@ -880,7 +912,7 @@ class Finder {
                 for (uint32_t i = 0; i < list_n; ++i) rank += sh.list[i] < mine;
             }
             __syncthreads();
-            if (threadIdx.x < list_n) sh.list[rank] = mine;
+            if (threadIdx.x < list_n && SBW_CHECKED(rank < list_n, SBW_SITE_GIVEN_SHARED)) sh.list[rank] = mine;
             __syncthreads();
             return;
         }
@@ -892,6 +924,7 @@ class Finder {
             for (uint32_t j = k >> 1; j > 0; j >>= 1) {
                 for (uint32_t t = threadIdx.x; t < len / 2; t += kGivenThreads) {
                     const uint32_t i = ((t & ~(j - 1)) << 1) | (t & (j - 1));
+                    if (!SBW_CHECKED(i + j < kListCap, SBW_SITE_GIVEN_SHARED)) continue;
                     const unsigned long long x = sh.list[i], y = sh.list[i + j];
                     if ((x > y) == ((i & k) == 0)) {
                         sh.list[i] = y;
@@ -952,7 +985,11 @@ __device__ __forceinline__ void narrow(const Settings &set, uint32_t &kept, unsi
     }
 }
 
+__device__ __forceinline__ void put_token(const GivenArgs &a, int64_t row, uint32_t col) {
+    if (SBW_CHECKED(row >= 0 && row < a.B && col < a.V, SBW_SITE_GIVEN_OUTPUT)) a.out_tokens[row] = static_cast<int32_t>(col);
+}
 __device__ __forceinline__ void answer(const GivenArgs &a, int64_t row, uint32_t kept, unsigned long long own, unsigned long long total) {
+    if (!SBW_CHECKED(row >= 0 && row < a.B, SBW_SITE_GIVEN_OUTPUT)) return;
     if (a.out_prob) a.out_prob[row] = total ? static_cast<float>(static_cast<double>(own) / static_cast<double>(total)) : 0.0f;
     if (a.out_kept) a.out_kept[row] = static_cast<int32_t>(kept);
 }
@@ -981,7 +1018,7 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
     }
     if (m == -INFINITY) {                                // nothing can be drawn: every CTA of the cluster sees it
         if (part == 0 && threadIdx.x == 0) {
-            a.out_tokens[r.row] = 0;
+            put_token(a, r.row, 0u);
             answer(a, r.row, 0u, 0ull, 0ull);
         }
         return;
@@ -1014,7 +1051,7 @@ __device__ __forceinline__ void by_weights(const GivenArgs &a, int64_t row, uint
         w = f.running;
     });
     if (threadIdx.x == 0) {
-        a.out_tokens[r.row] = static_cast<int32_t>(f.col);
+        put_token(a, r.row, f.col);
         answer(a, r.row, kept, f.own, total);
     }
     Command done = {};
@@ -1051,6 +1088,7 @@ __device__ __noinline__ void by_weights_rare(const GivenArgs &a, int64_t row, ui
 constexpr uint32_t kCodes = 8192;                        // magnitudes per sign
 constexpr uint32_t kFirstCode = (71u << 7) + 1u;         // the bits of the smallest magnitude, which is 2^-56 (1 + 2^-7)
 static_assert(2 * kCodes == 32 * kGivenThreads, "a thread per block of 32 places");
+static_assert(2 * kCodes * 4 == 1 << 16, "an offset of 16 bits stays within the counters");
 struct CodesShared {
     uint32_t n[2 * kCodes];                              // positive ones by magnitude, then negative ones
     unsigned long long block_weight[2 * kCodes / 32];    // of 32 places
@@ -1209,7 +1247,7 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
                 }
                 __syncthreads();
                 if (warp == 0) {
-                    const uint32_t place = sh.block * 32 + lane;
+                    const uint32_t place = (SBW_CHECKED(sh.block < 2 * kCodes / 32, SBW_SITE_GIVEN_SHARED) ? sh.block : 0u) * 32 + lane;
                     const uint32_t value = value_of_place(place);
                     const unsigned long long w = weight(value);
                     const uint32_t num = w ? sh.n[counter_of_place(place)] : 0u;
@@ -1328,7 +1366,7 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
             const uint32_t hits = hits_of(w[u], j);
             if (!hits) continue;
             mine += __popc(hits);
-            if (which == 0u) a.out_tokens[r.row] = static_cast<int32_t>(r.col0 + j * R::VEC + __ffs(hits) - 1);
+            if (which == 0u) put_token(a, r.row, r.col0 + j * R::VEC + __ffs(hits) - 1);
         }
     }
     if (which == 0u) return;
@@ -1363,7 +1401,7 @@ __global__ void __launch_bounds__(kGivenThreads, SCHEME == kSchemeNone ? 2 : 1) 
             continue;
         }
         if (to - own < left && left <= to)
-            a.out_tokens[r.row] = static_cast<int32_t>(r.col0 + j * R::VEC + __fns(hits, 0, static_cast<int>(left - (to - own))));
+            put_token(a, r.row, r.col0 + j * R::VEC + __fns(hits, 0, static_cast<int>(left - (to - own))));
         break;
     }
 }
@@ -1478,6 +1516,7 @@ extern "C" int sbw_sample_given(const void *logits, int dtype, int64_t B, int64_
     if (reinterpret_cast<uintptr_t>(logits) % (dtype == SBW_DTYPE_F32 ? 4 : 2) != 0) return SBW_ERR_INVALID_ARG;
     GivenArgs a = {};
     a.logits = logits;
+    a.B = B;
     a.V = V;
     a.ld = ld;
     a.vocab_offset = static_cast<uint32_t>(vocab_offset);

@@ -182,8 +182,15 @@ __device__ __forceinline__ uint32_t bf16_pair(Pair p) {
 // What a row's seed takes to make, as one number.
 template <int SCHEME>
 __device__ __forceinline__ uint64_t row_seed(const HeadArgs &a, int64_t row) {
+    if (!SBW_CHECKED(row >= 0 && row < a.B, SBW_SITE_HEAD_LOAD)) return 0ull;
     if constexpr (SCHEME == SBW_SCHEME_CONTEXT) return seed_context(a.bias.key, a.ctx + row * a.W, a.W);
     else return jenkins_min(a.ctx + row * a.W, a.W);
+}
+
+// A scale of a [rows, blocks of 128] array.
+__device__ __forceinline__ float load_scale(const HeadArgs &a, const float *p, const float *base, int64_t rows, int64_t ld) {
+    if (!SBW_CHECKED(lies_in_rows(p, 1, base, 4, rows, a.kblocks, ld), SBW_SITE_HEAD_LOAD)) return 0.0f;
+    return load_now(p);
 }
 
 // The green tests of a tile, made by the epilogue's warps while they wait for its products: at small B the weights'
@@ -288,16 +295,18 @@ __device__ __forceinline__ void store_rows(const HeadArgs &a, const uint32_t *st
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int r = warp + (i0 + u) * kEpilogueWarps;
-            if (r >= rows || !SBW_CHECKED(row0 + r < a.B, SBW_SITE_HEAD_STORE)) break;
+            if (r >= rows) break;
+            (void)SBW_CHECKED(r < kTileM, SBW_SITE_HEAD_SHARED);
             char *const at = base + r * stride;
             const uint32_t first = a.strided ? lane : lane * COLS, apart = a.strided ? 32 : 1;
             if (!a.strided && col0 + first + COLS <= a.V) {
-                *reinterpret_cast<uint2 *>(at + lane * 8) = w[u];
+                if (SBW_CHECKED(lies_in_rows(at + lane * 8, COLS, a.logits, ESIZE, a.B, a.V, a.ld), SBW_SITE_HEAD_STORE))
+                    *reinterpret_cast<uint2 *>(at + lane * 8) = w[u];
             } else {
 #pragma unroll
                 for (int i = 0; i < COLS; ++i) {
                     const uint32_t v = i < PER ? w[u].x : w[u].y, c = first + i * apart;
-                    if (col0 + c >= a.V) break;
+                    if (col0 + c >= a.V || !SBW_CHECKED(lies_in_rows(at + c * ESIZE, 1, a.logits, ESIZE, a.B, a.V, a.ld), SBW_SITE_HEAD_STORE)) break;
                     if constexpr (DTYPE == SBW_DTYPE_F32) reinterpret_cast<uint32_t *>(at)[c] = v;
                     else reinterpret_cast<uint16_t *>(at)[c] = static_cast<uint16_t>(v >> (16 * (i & 1)));
                 }
@@ -324,6 +333,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
     const uint32_t stage_bytes = kWBytes + kTileM * kBlock, copied = kWBytes + a.x_bytes;
     uint32_t *const staging = reinterpret_cast<uint32_t *>(
         dynamic_smem + (stages_at - smem_addr(dynamic_smem)) + a.stages * stage_bytes);
+    (void)SBW_CHECKED(lies_in_shared(staging, kStagingBytes, dynamic_smem), SBW_SITE_HEAD_SHARED);
     const uint32_t full = smem_addr(bars), empty = full + 8 * kMaxStages;
     const uint32_t ready = empty + 8 * kMaxStages, taken = ready + 8 * NBUF, last = taken + 8 * NBUF;
 
@@ -474,12 +484,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
             Pair acc[PART / 2];
 #pragma unroll
             for (int i = 0; i < PART / 2; ++i) acc[i] = 0ull;
-            float sx = load_now(xs), sw = load_now(ws);        // a block's scales are on their way while the one before is added
+            const int64_t w_rows = (static_cast<int64_t>(a.V) + kBlock - 1) / kBlock;
+            float sx = load_scale(a, xs, a.xs, a.B, a.ld_xs), sw = load_scale(a, ws, a.ws, w_rows, a.ld_ws);    // a block's scales are on their way while the one before is added
             for (uint32_t kb = 0; kb < a.kblocks; ++kb) {
                 const float s = sx * sw;
                 if (kb + 1 < a.kblocks) {
-                    sx = load_now(xs + kb + 1);
-                    sw = load_now(ws + kb + 1);
+                    sx = load_scale(a, xs + kb + 1, a.xs, a.B, a.ld_xs);
+                    sw = load_scale(a, ws + kb + 1, a.ws, w_rows, a.ld_ws);
                 }
                 greens.advance(a, staging, per_block, tile_col, warp - 4, lane);
                 if (ok) ok = __all_sync(0xffffffffu, barrier_wait(ready + 8 * buf, parity, gave_up, limit));
@@ -524,6 +535,7 @@ uint32_t r[2][16];
             for (int pass = 0; pass < kPasses; ++pass) {
                 if (rows && (kTogether > 1 ? wg / kTogether == pass : wg == pass / kSub)) {
                     uint32_t *const to = staging + (quarter * 32 + lane) * kRowStride + wg % kTogether * WORDS;
+                    (void)SBW_CHECKED(lies_in_shared(to, WORDS * 4, dynamic_smem), SBW_SITE_HEAD_SHARED);
 #pragma unroll
                     for (int i = 0; i < WORDS; i += 2) {
                         uint2 w;

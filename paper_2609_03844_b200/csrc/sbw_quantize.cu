@@ -62,17 +62,21 @@ struct Elements {
     }
     // Elements col .. col + VEC - 1 of a row; those from K on are 0.
     template <bool VECTOR>
-    __device__ __forceinline__ void load(const void *row_ptr, int64_t col, int64_t K) {
+    __device__ __forceinline__ void load(const QuantArgs &a, int64_t row, int64_t col) {
+        constexpr int ESIZE = 16 / VEC;
+        const char *const row_ptr = static_cast<const char *>(a.x) + row * a.ld * ESIZE;
         w = make_uint4(0u, 0u, 0u, 0u);
-        if (VECTOR && col + VEC <= K) {
-            w = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const char *>(row_ptr) + col * (16 / VEC)));
+        if (VECTOR && col + VEC <= a.K) {
+            const char *const p = row_ptr + col * ESIZE;
+            if (SBW_CHECKED(lies_in_rows(p, VEC, a.x, ESIZE, a.R, a.K, a.ld), SBW_SITE_QUANT_LOAD)) w = __ldcs(reinterpret_cast<const uint4 *>(p));
         } else {
             uint32_t *e = reinterpret_cast<uint32_t *>(&w);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                if (col + i >= K) continue;
-                if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = static_cast<const uint32_t *>(row_ptr)[col + i];
-                else e[i >> 1] |= static_cast<uint32_t>(static_cast<const uint16_t *>(row_ptr)[col + i]) << (16 * (i & 1));
+                const char *const p = row_ptr + (col + i) * ESIZE;
+                if (col + i >= a.K || !SBW_CHECKED(lies_in_rows(p, 1, a.x, ESIZE, a.R, a.K, a.ld), SBW_SITE_QUANT_LOAD)) continue;
+                if constexpr (DTYPE == SBW_DTYPE_F32) e[i] = *reinterpret_cast<const uint32_t *>(p);
+                else e[i >> 1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p)) << (16 * (i & 1));
             }
         }
     }
@@ -90,7 +94,8 @@ struct Elements {
     }
     // Writes the codes of the elements that exist.
     template <bool VECTOR, bool PLAIN>
-    __device__ __forceinline__ void store(uint8_t *row_out, int64_t col, int64_t K, const Divisor &d) const {
+    __device__ __forceinline__ void store(const QuantArgs &a, int64_t row, int64_t col, const Divisor &d) const {
+        uint8_t *const row_out = a.out + row * a.ld_out;
         uint32_t code[VEC / 4];
 #pragma unroll
         for (int i = 0; i < VEC / 4; ++i) {
@@ -100,13 +105,15 @@ struct Elements {
                 make_float2(d.of<PLAIN>(at(4 * i + 2)), d.of<PLAIN>(at(4 * i + 3))), __NV_SATFINITE, __NV_E4M3);
             code[i] = static_cast<uint32_t>(lo) | static_cast<uint32_t>(hi) << 16;
         }
-        if (VECTOR && col + VEC <= K) {
+        if (VECTOR && col + VEC <= a.K) {
+            if (!SBW_CHECKED(lies_in_rows(row_out + col, VEC, a.out, 1, a.R, a.K, a.ld_out), SBW_SITE_QUANT_STORE)) return;
             if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(row_out + col) = make_uint2(code[0], code[1]);
             else *reinterpret_cast<uint32_t *>(row_out + col) = code[0];
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
-                if (col + i < K) row_out[col + i] = static_cast<uint8_t>(code[i >> 2] >> (8 * (i & 3)));
+                if (col + i < a.K && SBW_CHECKED(lies_in_rows(row_out + col + i, 1, a.out, 1, a.R, a.K, a.ld_out), SBW_SITE_QUANT_STORE))
+                    row_out[col + i] = static_cast<uint8_t>(code[i >> 2] >> (8 * (i & 3)));
         }
     }
 };
@@ -114,6 +121,11 @@ struct Elements {
 __device__ __forceinline__ float scale_of(uint32_t amax_bits) {
     const float s = __fdiv_rn(__uint_as_float(amax_bits), 448.0f);
     return s < 0x1p-126f ? 0x1p-126f : s;       // a NaN stays one
+}
+
+__device__ __forceinline__ void store_scale(const QuantArgs &a, int64_t row, uint32_t kb, float s, int block_rows) {
+    float *const p = a.scales + row * a.ld_scales + kb;
+    if (SBW_CHECKED(lies_in_rows(p, 1, a.scales, 4, (a.R + block_rows - 1) / block_rows, a.kblocks, a.ld_scales), SBW_SITE_QUANT_STORE)) *p = s;
 }
 
 // Blocks of one row: LANES threads per block, kUnroll blocks at a time so that as many loads are in
@@ -140,8 +152,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
             kb[u] = real[u] ? static_cast<uint32_t>(b - row[u] * a.kblocks) : 0;
             e[u].w = make_uint4(0u, 0u, 0u, 0u);
             if (real[u])
-                e[u].template load<VECTOR>(static_cast<const char *>(a.x) + row[u] * a.ld * (16 / E::VEC),
-                                           static_cast<int64_t>(kb[u]) * kBlock + part * E::VEC, a.K);
+                e[u].template load<VECTOR>(a, static_cast<int64_t>(row[u]), static_cast<int64_t>(kb[u]) * kBlock + part * E::VEC);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
@@ -151,11 +162,11 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const Quan
             if (!real[u]) continue;
             const float s = scale_of(m);
             const Divisor d(s);
-            uint8_t *const to = a.out + row[u] * a.ld_out;
+            const int64_t r = static_cast<int64_t>(row[u]);
             const int64_t col = static_cast<int64_t>(kb[u]) * kBlock + part * E::VEC;
-            if (d.plain) e[u].template store<VECTOR, true>(to, col, a.K, d);
-            else e[u].template store<VECTOR, false>(to, col, a.K, d);
-            if (part == 0) a.scales[row[u] * a.ld_scales + kb[u]] = s;
+            if (d.plain) e[u].template store<VECTOR, true>(a, r, col, d);
+            else e[u].template store<VECTOR, false>(a, r, col, d);
+            if (part == 0) store_scale(a, r, kb[u], s, 1);
         }
     }
 }
@@ -177,7 +188,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_tiles_kernel(const Qua
     for (int i = 0; i < kSteps; ++i) {
         const int64_t row = row0 + i * kRowsAtOnce;
         e[i].w = make_uint4(0u, 0u, 0u, 0u);
-        if (row < a.R) e[i].template load<VECTOR>(static_cast<const char *>(a.x) + row * a.ld * (16 / E::VEC), col, a.K);
+        if (row < a.R) e[i].template load<VECTOR>(a, row, col);
     }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) m = max(m, e[i].largest());
@@ -192,12 +203,12 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_tiles_kernel(const Qua
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int64_t row = row0 + i * kRowsAtOnce;
-            if (row < a.R) e[i].template store<VECTOR, decltype(plain)::value>(a.out + row * a.ld_out, col, a.K, d);
+            if (row < a.R) e[i].template store<VECTOR, decltype(plain)::value>(a, row, col, d);
         }
     };
     if (d.plain) store(std::true_type{});
     else store(std::false_type{});
-    if (threadIdx.x == 0) a.scales[rb * a.ld_scales + kb] = s;
+    if (threadIdx.x == 0) store_scale(a, rb, kb, s, kBlock);
 }
 
 template <int DTYPE, bool VECTOR>
