@@ -53,9 +53,11 @@ constexpr int kCountingSort = 128;         // a list up to this length is sorted
 constexpr int kPrefixCap = 1024;           // a list from the first candidate on is made up to this length
 constexpr int kMaxParts = 8;
 constexpr int64_t kMaxGivenV = 320 * 1024;
-constexpr int64_t kSliceBytes = 68 * 1024;           // of a row in a CTA's shared memory, before more CTAs share it
+// Of a resident row in a CTA's shared memory, before more CTAs share it.  The size hardly matters, as the hash takes the time
+// however the row is shared out: 64 x 128256 fp32 watermarked 123 us with 34 or 68 KB, 121 with 136; 256 x 151936 467 with each.
+constexpr int64_t kSliceBytes = 68 * 1024;
 // A sum of 17 bits holds 32768 candidates: of a resident part every other warp has its own, of a streamed row every warp.
-static_assert(kMaxGivenV / kMaxParts / 2 + 8 * kGivenThreads <= 32768 && kSliceBytes / 2 / 2 + 8 * kGivenThreads <= 32768, "");
+static_assert(kMaxGivenV / kMaxParts / 2 + 8 * kGivenThreads <= 32768 && kSliceBytes / 4 / 2 + 8 * kGivenThreads <= 32768, "");
 static_assert(kMaxGivenV / kGivenWarps + 8 * 32 + 16 <= 32768, "");
 constexpr uint32_t kLimb = 12;                       // of a split's two sums
 
@@ -319,9 +321,10 @@ struct Row {
     static constexpr int DTYPE = DTYPE_, SCHEME = SCHEME_;
     static constexpr bool RESIDENT = RESIDENT_;
     static constexpr int VEC = DTYPE == SBW_DTYPE_F32 ? 4 : 8;
+    static_assert(!RESIDENT || DTYPE == SBW_DTYPE_F32, "");
     using Shared = GivenShared<RESIDENT ? 2 : kGivenWarps>;
     // loads in flight per thread
-    static constexpr int kInFlight = RESIDENT && SCHEME == kSchemeNone ? 8 : SCHEME == kSchemeNone ? 4 : 2;
+    static constexpr int kInFlight = SCHEME == kSchemeNone ? 4 : 2;
 
     const GivenArgs &a;
     int64_t row;
@@ -438,8 +441,7 @@ struct Row {
         float x;
         if constexpr (RESIDENT) {
             if (!SBW_CHECKED(lies_in_shared(slice + j, 16, room_base()), SBW_SITE_GIVEN_SHARED)) return -INFINITY;
-            x = DTYPE == SBW_DTYPE_F32 ? reinterpret_cast<const float *>(slice + j)[i]
-                                       : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(slice + j)[i]);
+            x = reinterpret_cast<const float *>(slice + j)[i];
         } else {
             const uint32_t col = col0 + j * VEC + i;
             if (!SBW_CHECKED(lies_here(row_ptr + static_cast<int64_t>(col) * (16 / VEC), 1), SBW_SITE_GIVEN_LOAD)) return -INFINITY;

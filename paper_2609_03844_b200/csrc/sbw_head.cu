@@ -37,7 +37,7 @@ constexpr int kBlock = 128;            // columns of the operands per scale, and
 constexpr int kTileM = 128;
 constexpr int kHeadThreads = 384;
 constexpr int kEpilogueWarps = 8;
-constexpr int kMaxStages = 16;
+constexpr int kMaxStages = 6;                        // of narrow tiles; 4 of wide ones
 constexpr int kTmemColumns = 512;
 constexpr uint64_t kWaitLimit = 2000000000ull;      // nanoseconds
 constexpr uint64_t kLongestLook = 10000000ull;      // more than that between two looks at the clock is time switched out
@@ -46,6 +46,9 @@ constexpr int kRowStride = kRowWords + 2;            // 8-byte accesses by row a
                                                      // two words behind a row hold its watermark seed
 constexpr int kStagingBytes = kTileM * kRowStride * 4;
 constexpr int kMaxDynamicBytes = 227 * 1024 - 1024;  // what a CTA can have less the barriers
+// Stages of tiles of n columns beside the staging area and what aligning them takes.
+constexpr int stages_of(int n) { return (kMaxDynamicBytes - 1024 - kStagingBytes) / ((n + kTileM) * kBlock); }
+static_assert(stages_of(128) == kMaxStages && stages_of(256) == 4, "");
 
 struct HeadArgs {
     const float *xs, *ws;
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BN + wg * PART;
                 const Pair both = pair_of(__float_as_uint(s), __float_as_uint(s));
-uint32_t r[2][16];
+                uint32_t r[2][16];
                 if (rows) read_columns(r[0], from);
 #pragma unroll
                 for (int c = 0; c < PART / 16; ++c) {
@@ -610,8 +613,7 @@ int launch_head(HeadArgs &a, const void *x, int64_t ld_x, const void *w, int64_t
     const int box_m = a.B < kTileM ? static_cast<int>((a.B + 7) / 8 * 8) : kTileM;
     a.x_bytes = static_cast<uint32_t>(box_m) * kBlock;
     const uint32_t stage_bytes = BN * kBlock + kTileM * kBlock;
-    a.stages = (kMaxDynamicBytes - 1024 - kStagingBytes) / stage_bytes;
-    if (a.stages > kMaxStages) a.stages = kMaxStages;
+    a.stages = stages_of(BN);
     const size_t bytes = 1024 + a.stages * stage_bytes + kStagingBytes;
     a.m_tiles = (a.B + kTileM - 1) / kTileM;
     constexpr int kEsize = DTYPE == SBW_DTYPE_F32 ? 4 : 2;
