@@ -211,3 +211,33 @@ def test_values_around_zero(dtype):
     wide = x[:4].repeat(60, 1)                          # a CTA per row
     u = np.random.default_rng(9).random(240, dtype=np.float32)
     compare(wide, u, np.ones(240, np.float32))
+
+
+def test_bins_keep_the_order():
+    """The sampler's bins are the weights' fp32 bits from the 17th up.  The polynomial of the weights, fused as they are, over every
+    fp32 argument from 0 down to -40: a smaller argument never lies in a higher bin."""
+    require_gpu()
+
+    def fma(a, b, c):
+        """a b + c of fp32 values, rounded once: the sum in fp64 rounded to odd, then to fp32."""
+        p, c = a.double() * b.double(), torch.full_like(b, c, dtype=torch.float64)
+        s = p + c
+        part = s - p
+        rest = (p - (s - part)) + (c - part)
+        bits = s.view(torch.int64)
+        toward = torch.where((rest > 0) == (s > 0), 1, -1)
+        even = (bits & 1) == 0
+        return torch.where((rest != 0) & even, bits + toward, bits).view(torch.float64).float()
+
+    step, last = 1 << 25, None
+    end = int(np.float32(40).view(np.int32)) + 1
+    for at in range(0, end, step):
+        y = -torch.arange(at, min(at + step, end), dtype=torch.int32, device="cuda").view(torch.float32)
+        n = y.round()
+        f = y - n
+        p = torch.full_like(f, float(given._EXP2[0]))
+        for a in given._EXP2[1:]:
+            p = fma(p, f, float(a))
+        bins = ((p.view(torch.int32).long() + (n.long() << 23)) >> 17)
+        assert bool((bins[1:] <= bins[:-1]).all()) and (last is None or int(bins[0]) <= last)
+        last = int(bins[-1])

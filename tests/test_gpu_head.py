@@ -253,3 +253,36 @@ def test_quantizer_keeps_the_sign_of_zero(block_rows, dtype):
         s = torch.empty(-(-R // block_rows), blocks(K), device="cuda")
         sbw.sbw_quantize_fp8(src[:, :K], out.view(E4M3)[:, :K], s, block_rows=block_rows)
         assert torch.equal(out[:, :K].cpu(), want)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quotients_next_to_the_borders_of_codes(block_rows):
+    """x within two steps of what lies half-way between two codes, times the scale: where a quotient that is not the rounded one
+    gives another code.  Scales over their whole range, the ends of the one in which quotients are three operations among them."""
+    require_gpu()
+    import paper_2609_03844_b200 as sbw
+
+    g = torch.Generator().manual_seed(12)
+    R, K = 512, 1024
+    values = torch.arange(0x7F, dtype=torch.uint8).view(E4M3).float()              # 0 .. 448
+    middles = ((values[1:] + values[:-1]) / 2).numpy()
+    exponent = torch.randint(-118, 110, (R, K // 128), generator=g).float()
+    exponent[:8] = torch.tensor([-91.0, -90, -89, -88, 88, 89, 90, 91])[:, None]
+    if block_rows == 128:
+        exponent = exponent[:, :].view(4, 128, -1)[:, :1].expand(4, 128, -1).reshape(R, -1)
+    top = (torch.rand(R, K // 128, generator=g) + 1) * 448 * torch.exp2(exponent)
+    if block_rows == 128:
+        top = top.view(4, 128, -1)[:, :1].expand(4, 128, -1).reshape(R, -1)
+    top = top.numpy().astype(np.float32)
+    scale = top / np.float32(448)
+    pick = torch.randint(0, len(middles), (R, K), generator=g).numpy()
+    x = (middles[pick].astype(np.float64) * np.repeat(scale, 128, 1)).astype(np.float32)
+    x = (x.view(np.int32) + torch.randint(-2, 3, (R, K), generator=g).numpy().astype(np.int32)).view(np.float32)
+    x *= np.where(torch.rand(R, K, generator=g).numpy() < 0.5, np.float32(-1), np.float32(1))
+    x[:, ::128] = top                                                               # the largest magnitude of its block
+    assert np.all(np.abs(x) <= np.repeat(top, 128, 1))
+    want = torch.from_numpy(np.clip(x / np.repeat(scale, 128, 1), -448, 448)).to(E4M3).view(torch.uint8)
+    q, s = torch.empty(R, K, dtype=E4M3, device="cuda"), torch.empty(R // block_rows, K // 128, device="cuda")
+    sbw.sbw_quantize_fp8(torch.from_numpy(x).cuda(), q, s, block_rows=block_rows)
+    assert np.array_equal(s.cpu().numpy(), scale[::block_rows])
+    assert torch.equal(q.view(torch.uint8).cpu(), want)
