@@ -488,7 +488,7 @@ int sbw_detect_weighted(const int32_t *tokens, const float *weights, const int32
  * summed in fp32 (a block's sum on the tensor cores, the blocks in order by fused multiply-add with the product
  * of the two scales), rounded once to `dtype`; green logits then get delta as in sbw_bias_logits: the result has
  * the bits of sbw_head_logits with delta 0 followed by sbw_bias_logits.
- *   x           device, [B, ld_x] e4m3 codes, 16-byte aligned, ld_x >= K a multiple of 16 (any value where B is 1);
+ *   x           device, [B, ld_x] e4m3 codes, 16-byte aligned, ld_x >= K a multiple of 16 (any from K on where B is 1);
  *               x_scales device [B, ld_x_scales] float, ld_x_scales >= ceil(K / 128).
  *   w           device, [V, ld_w] e4m3 codes, one row per vocabulary entry, aligned likewise;
  *               w_scales device [ceil(V / 128), ld_w_scales] float.

@@ -8,10 +8,11 @@
 // question, asked up to three times per row: at which candidate does the running number (top-k) or the
 // running weight (top-p, then the draw) reach a target?
 //
-// A row belongs to one CTA, or to a cluster of up to 8 where there are fewer rows than SMs.  Two ways of doing it:
+// A row belongs to one CTA, or to a cluster of up to 8 where that many CTAs for every row are under way at once, and, watermarked
+// in fp32, where a CTA has no room for its part (from 17408 logits on: 128256 are 8 CTAs at any batch).  Two ways of doing it:
 //   by value    (bf16) few values are distinct: one pass counts them, before the maximum is known; weights and all three
 //               questions are then a matter of the counters, and a second pass, from L2, finds the column.
-//   by weight   (fp32, and the rare bf16 rows that the counters do not hold)
+//   by weight   (fp32, and the bf16 rows that the counters do not hold, such as those with a maximum around 0)
 //     maximum    one pass
 //     histogram  1024 bins by the weight's exponent and six bits of its mantissa, down to 2^-16 of the maximum: the
 //                number of candidates and the sum of the other 17 bits (32-bit counters, native adds).  Weights below
@@ -20,10 +21,14 @@
 //                for (of that bin alone if those are too many for the list), sorts them and walks the running sums.  The
 //                first list usually answers all questions.
 //     A bin too full for the list is split by the candidates' bits, 1024 ways at a time; candidates of equal value,
-//     however many, are counted by column.  Plain rows are read again by every pass; watermarked ones stay in the
-//     cluster's shared memory, since the hash costs more than a pass.
-// Bound (1024 x 128256): bf16 by the integer pipe and the adds to shared memory of the counting pass, 166 us where the bytes
-// take 40; fp32 by the three readings of rows that L2 does not hold, 420 us where the bytes take 80.
+//     however many, are counted by column.  Rows are read again by every pass, watermarked bf16 ones hashed again;
+//     watermarked fp32 ones stay in the cluster's shared memory.
+// Measured on 1024 x 128256, repeated calls: bf16 166 us, where the bytes take 40; the counting pass's 21 instructions for 32
+// logits, half of them on the ALU pipe, and its adds to shared memory bound it.  fp32 with top-p 0.9 422 us, where the bytes take 80
+// and the three readings, of rows that L2 does not hold, 240; the passes' instructions (45 for 32 logits) and a row's serial
+// phases are the rest.  A row that draws a candidate below 2^-16 of its maximum is slow, since a split of the tail handles each of
+// its candidates by itself: 256 x 128256 with no filter 97 us with every random number 0.5, 967 where one is 0.99999.  bf16 rows
+// with a maximum of 0 are counted first and then done by weight: 1024 x 128256 403 us with top-p 0.9.
 #include <atomic>
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -53,8 +58,8 @@ constexpr int kCountingSort = 128;         // a list up to this length is sorted
 constexpr int kPrefixCap = 1024;           // a list from the first candidate on is made up to this length
 constexpr int kMaxParts = 8;
 constexpr int64_t kMaxGivenV = 320 * 1024;
-// Of a resident row in a CTA's shared memory, before more CTAs share it.  The size hardly matters, as the hash takes the time
-// however the row is shared out: 64 x 128256 fp32 watermarked 123 us with 34 or 68 KB, 121 with 136; 256 x 151936 467 with each.
+// Of a resident row in a CTA's shared memory, before more CTAs share it.  The size hardly matters: 64 x 128256 fp32
+// watermarked takes 123 us with 34 or 68 KB and 121 with 136, 256 x 151936 467 with each.
 constexpr int64_t kSliceBytes = 68 * 1024;
 // A sum of 17 bits holds 32768 candidates: of a resident part every other warp has its own, of a streamed row every warp.
 static_assert(kMaxGivenV / kMaxParts / 2 + 8 * kGivenThreads <= 32768 && kSliceBytes / 4 / 2 + 8 * kGivenThreads <= 32768, "");

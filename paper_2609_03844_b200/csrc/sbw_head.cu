@@ -16,9 +16,11 @@
 // call and the matrix unit's time for rows that are not there is hidden behind them.  (With the sides
 // exchanged every thread needs a scale per column and block from shared memory.)
 //
-// Bound: up to 128 rows the weights' bytes (1 x 128256 x 4096: 89 us in short runs, 5.9 TB/s; long ones are held back by the
-// 1000 W cap, 109); above, the fp32 sums of the epilogue's warps beside the products (2048 x 128256 x 4096: 1.08 ms in short
-// runs, 1.28 under the cap; the products alone take 0.65, with the copies 0.77).
+// Bound: up to 128 rows the weights' bytes, and in repeated calls the 1000 W cap (1 x 128256 x 4096: 109 us, 4.8 TB/s; 90 us, 5.8
+// TB/s in short runs, which the cap does not hold back); above, the fp32 sums of the epilogue's warps beside the products
+// (2048 x 128256 x 4096: 1.29 ms, 1.10 in short runs; the products alone take 0.65, with the copies 0.77).  There is one
+// CTA per tile of 128 or 256 columns and no split along K, so few columns leave SMs idle: 4096 columns for up to 128 rows are 32
+// tiles (24 x 4096 x 128256: 357 us, where the bytes take 81), 1000 are 8 (1 x 1000 x 8192: 26 us).
 //
 // Every wait is bounded: one that does not end within kWaitLimit gives up, the rest of the CTA's logits are NaN, the kernel
 // returns, and sbw_head_gave_up tells of it.
